@@ -50,6 +50,7 @@ extern "C" {
 
 #define HERO_DTYPE_FP32 0
 #define HERO_DTYPE_BF16 1
+#define HERO_DTYPE_E4M3 2   /* 8 bits: 4 of exponent, 3 of mantissa, largest value 448; with block scales (hero_gemm_fp8 and what feeds it) */
 
 typedef struct hero_ctx hero_ctx;   /* opaque */
 
@@ -259,6 +260,43 @@ int hero_attention_bf16_safe(const void *d_q, const void *d_k, const void *d_v, 
 int hero_attention_bf16_q_scaled(const void *d_q, const void *d_k, const void *d_v, void *d_o,
                                  int B, int n_q, int N, int heads, void *stream);
 
+/* ---- 8-bit operands with a scale for each block of 128 (stateless; the paper has no counterpart) ---
+ * The refresh path's linear layers with operands in e4m3: what writes such operands and the product that reads them.
+ * A matrix [rows, cols] is held as e4m3 bytes, row-major and compact, and fp32 scales, row-major and compact, one per block:
+ *   activations  blocks of 1 x 128,   scales [rows, ceil(cols / 128)]
+ *   weights      blocks of 128 x 128, scales [ceil(rows / 128), ceil(cols / 128)]
+ * (the last block of a row or column may be smaller).  A block is stored as q = e4m3(v * (1 / s)), to nearest, ties to even, with
+ * s = max(amax * fp32(1 / 448), 2^-126) and amax its largest magnitude; q * s is what it stands for.  A block that holds an
+ * infinity or a NaN gets a NaN for its scale and for every value.  Columns of e4m3 matrices are a multiple of 16
+ * (HERO_ERR_ALIGN otherwise); e4m3 and run-dtype pointers are 16-byte aligned, scales 4-byte.  `dtype` is the run dtype (fp32 or
+ * bf16) of the inputs.  Argument errors are reported before anything is launched; no rows at all is HERO_OK.
+ * hero_gemm_fp8 sets up its status word (a cudaMalloc, see hero_gemm_bf16) on its first call on a device: make that call before any
+ * stream capture.  Calls share nothing else, so they may overlap on several streams. */
+
+/* d_x [rows, cols] to d_q and d_scale, blocks of block_rows x 128 (block_rows 1 or 128). */
+int hero_quantize_fp8(const void *d_x, void *d_q, float *d_scale, int rows, int cols, int block_rows, int dtype, void *stream);
+/* hero_gather_ln_modulate with its result as an e4m3 operand: d_out [B,n_sel,D], d_out_scale [B,n_sel,ceil(D/128)].  The other
+ * arguments as there; D is at most 12288. */
+int hero_gather_ln_modulate_fp8(const void *d_x, const void *d_add, const int *d_idx, const float *d_shift, const float *d_scale,
+                                int mod_ld, void *d_out, float *d_out_scale, int B, int N, int n_sel, int D, int dtype, void *stream);
+/* Root-mean-square norm with the residual's addition, for base models whose blocks use it in LayerNorm's place:
+ * h = x + add, d_sum = h (rounded to dtype), d_out = h / sqrt(mean(h^2) + eps) * gain (of the unrounded h), statistics in fp32.
+ * d_x, d_add, d_sum, d_out are [rows, D], d_gain is [D], all in dtype; d_add, d_gain and d_sum may be NULL (nothing added, a gain
+ * of 1, the sum not kept).  d_sum may be d_x or d_add, d_out may be d_x or d_add, but not both the same.  D is a multiple of 8
+ * (bf16) or 4 (fp32) and at most 12288; eps is not negative.  A row of zeros with eps = 0 is NaN. */
+int hero_rms_norm(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, int rows, int D, float eps,
+                  int dtype, void *stream);
+/* The same with the norm's result as an e4m3 operand (d_out [rows, D] is not d_x or d_add; D is a multiple of 16). */
+int hero_rms_norm_fp8(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, float *d_out_scale, int rows,
+                      int D, float eps, int dtype, void *stream);
+/* C[M,N] = act(A[M,K] W[N,K]^T + bias[N]): A with blocks of 1 x 128 (d_a_scale [M,ceil(K/128)]), W with blocks of 128 x 128
+ * (d_w_scale [ceil(N/128),ceil(K/128)]); the sum over a block of 128 on the tensor cores, scaled and added up over the blocks in
+ * fp32.  bias is bf16 or NULL; act = 1 applies GELU-tanh.  out_dtype: HERO_DTYPE_BF16, HERO_DTYPE_FP32 (any N; d_c_scale NULL), or
+ * HERO_DTYPE_E4M3 (N a multiple of 16), which writes C as an operand of the next product, d_c_scale [M,ceil(N/128)], quantised from
+ * the fp32 result.  Every wait on the device is bounded, as in hero_gemm_bf16; hero_isolated_status reports one that gave up. */
+int hero_gemm_fp8(const void *d_a, const float *d_a_scale, const void *d_w, const float *d_w_scale, const void *d_bias, void *d_c,
+                  float *d_c_scale, int M, int N, int K, int act, int out_dtype, void *stream);
+
 /* hero_attention_bf16 without any allocation (the paper has no counterpart: this entry point
  * exists for the sake of callers, not of the method).  hero_attention_bf16 obtains its status
  * word with cudaMalloc on first use; a caller that must never enter the CUDA allocator - a
@@ -287,7 +325,7 @@ int hero_attention_bf16_static(const void *d_q, const void *d_k, const void *d_v
  * up; n_records <= 16384).  Returns HERO_ERR_TIMEOUT if the count is not 0.  The paper has no counterpart. */
 int hero_attention_bf16_static_status(void *stream, int *h_gave_up, int *h_records, int n_records);
 
-/* Synchronise `stream` and return HERO_ERR_TIMEOUT if hero_gemm_bf16 / hero_attention_bf16 gave
+/* Synchronise `stream` and return HERO_ERR_TIMEOUT if hero_gemm_bf16 / hero_gemm_fp8 / hero_attention_bf16 gave
  * up on a bounded device-side wait since the last poll, else HERO_OK.  The word that is polled lives
  * on the device that is current at the call (one per device). */
 int hero_isolated_status(void *stream);
@@ -309,6 +347,9 @@ int hero_plan_fp32_gemm(int M, int N, int K, int sms, int *tile, int *ctas);
 /* The bf16 GEMM (of a context and hero_gemm_bf16; qk = 1: a QKV projection that treats q and k rows as well): tiles of *columns
  * columns, 128 rows in a cluster of *ctas thread blocks that share K, or, *ctas 0, 256 rows on a pair of thread blocks. */
 int hero_plan_bf16_gemm(int M, int N, int K, int qk, int sms, int *columns, int *ctas);
+/* hero_gemm_fp8 (e4m3_out: 1 for results in e4m3): tiles of 128 rows of A, or with *swap 1 of 128 rows of W, by *columns rows of the
+ * other operand in a cluster of *ctas thread blocks that share K; or, *ctas 0, 256 rows of A by *columns on a pair of thread blocks. */
+int hero_plan_fp8_gemm(int M, int N, int K, int e4m3_out, int sms, int *columns, int *ctas, int *swap);
 /* The fp32 attention of a context, n_q queries against N keys: the keys of 32 queries of a head are shared by a cluster of
  * *ctas thread blocks. */
 int hero_plan_fp32_attention(int B, int n_q, int N, int heads, int head_dim, int sms, int *ctas);

@@ -15,7 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhero.so")
 
 OK, ERR_ARG, ERR_ALIGN, ERR_CAP, ERR_STATE, ERR_CUDA, ERR_TIMEOUT, ERR_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 STATE = dict(ages=0, calls=1, k=2, v=3, g_attn=4, g_ffn=5, g_attn_prev=6, g_ffn_prev=7, steps=8, stack_last=9,
              stack_prev=10)
 
@@ -28,6 +28,7 @@ EXPORTS = [
     "hero_gather_rows", "hero_scatter_rows", "hero_gemm_bf16", "hero_attention_bf16", "hero_attention_bf16_safe", "hero_attention_bf16_q_scaled", "hero_attention_bf16_static", "hero_attention_bf16_static_status",
     "hero_isolated_status", "hero_selftest_wait_timeout", "hero_gather_ln_modulate",
     "hero_plan_fp32_gemm", "hero_plan_fp32_attention", "hero_plan_bf16_gemm",
+    "hero_quantize_fp8", "hero_gather_ln_modulate_fp8", "hero_rms_norm", "hero_rms_norm_fp8", "hero_gemm_fp8", "hero_plan_fp8_gemm",
     "hero_state_get", "hero_state_set", "hero_second_difference_moments", "hero_extrapolation_error",
 ]
 
@@ -102,6 +103,12 @@ def load() -> C.CDLL:
         "hero_gather_ln_modulate": (i, [vp, vp, vp, vp, vp, i, vp, i, i, i, i, i, vp]),
         "hero_second_difference_moments": (i, [vp, vp, vp, ll, i, vp, vp]),
         "hero_extrapolation_error": (i, [vp, vp, vp, ll, i, i, i, vp, vp]),
+        "hero_quantize_fp8": (i, [vp, vp, vp, i, i, i, i, vp]),
+        "hero_gather_ln_modulate_fp8": (i, [vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, i, vp]),
+        "hero_rms_norm": (i, [vp, vp, vp, vp, vp, i, i, C.c_float, i, vp]),
+        "hero_rms_norm_fp8": (i, [vp, vp, vp, vp, vp, vp, i, i, C.c_float, i, vp]),
+        "hero_gemm_fp8": (i, [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp]),
+        "hero_plan_fp8_gemm": (i, [i, i, i, i, i, ip, ip, ip]),
         "hero_plan_fp32_gemm": (i, [i, i, i, i, ip, ip]),
         "hero_plan_bf16_gemm": (i, [i, i, i, i, i, ip, ip]),
         "hero_plan_fp32_attention": (i, [i, i, i, i, i, i, ip]),
@@ -377,6 +384,124 @@ def hero_attention_bf16_static_status(n_records: int = 0):
     return gave_up.value, list(rec)[:n_records]
 
 
+# ---- 8-bit operands with a scale for each block of 128 ------------------------------
+F8 = torch.float8_e4m3fn
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def _f8_call(name: str, tensors: dict, args: tuple) -> None:
+    """Check {argument name: (tensor or None, dtype, shape)} and call `name` with `args` and the current stream of the tensors' device.
+
+    Every tensor is contiguous, of the named dtype and shape and on one GPU, which need not be the current one; a HeroError with
+    ERR_ARG says which is not."""
+    device = None
+    for arg, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise HeroError(ERR_ARG, f"{name}: {arg} must be a CUDA tensor")
+        if device is None:
+            device = t.device
+        if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise HeroError(ERR_ARG, f"{name}: {arg} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                                     f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(getattr(load(), name)(*args, _stream()), name)
+    else:
+        _check(getattr(load(), name)(*args, _stream()), name)
+
+
+def _matrix(name: str, arg: str, t, dims: int = 2):
+    if t is None or t.dim() != dims:
+        raise HeroError(ERR_ARG, f"{name}: {arg} must be a {dims}-dimensional tensor")
+    return t.shape
+
+
+def _run_dtype(name: str, t) -> int:
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise HeroError(ERR_ARG, f"{name}: inputs are bf16 or fp32, got {t.dtype}")
+    return DTYPE_BF16 if t.dtype == torch.bfloat16 else DTYPE_FP32
+
+
+def hero_quantize_fp8(x, q, scale, block_rows: int = 1):
+    """q (float8_e4m3fn), scale (fp32) <- x [rows, cols], a scale per row and 128 columns (block_rows=1) or per 128 x 128 elements."""
+    rows, cols = _matrix("hero_quantize_fp8", "x", x)
+    dtype = _run_dtype("hero_quantize_fp8", x)
+    _f8_call("hero_quantize_fp8",
+             {"x": (x, x.dtype, (rows, cols)), "q": (q, F8, (rows, cols)),
+              "scale": (scale, torch.float32, (rows if block_rows == 1 else _blocks(rows), _blocks(cols)))},
+             (_ptr(x), _ptr(q), _ptr(scale), rows, cols, block_rows, dtype))
+    return q, scale
+
+
+def hero_gather_ln_modulate_fp8(x, add, idx, shift, scale, out, out_scale):
+    """hero_gather_ln_modulate with its result in e4m3: out (float8_e4m3fn) [B, n_sel, D], out_scale [B, n_sel, ceil(D / 128)].
+    shift and scale are fp32 [B, D] with one row stride (they may be slices of one tensor); idx is int32 [n_sel] or None (the
+    first n_sel rows), its entries from 0 to N - 1."""
+    name = "hero_gather_ln_modulate_fp8"
+    B, N, D = _matrix(name, "x", x, 3)
+    n_sel = _matrix(name, "out", out, 3)[1]
+    dtype = _run_dtype(name, x)
+    for arg, t in (("shift", shift), ("scale", scale)):
+        if t is None or t.dtype != torch.float32 or tuple(t.shape) != (B, D) or t.device != x.device or (D > 1 and t.stride(1) != 1):
+            raise HeroError(ERR_ARG, f"{name}: {arg} must be fp32 of shape {(B, D)} on {x.device} with contiguous rows")
+    if B > 1 and shift.stride(0) != scale.stride(0):
+        raise HeroError(ERR_ARG, f"{name}: shift and scale must have the same row stride")
+    _f8_call(name, {"x": (x, x.dtype, (B, N, D)), "add": (add, x.dtype, (B, N, D)), "idx": (idx, torch.int32, (n_sel,)),
+                    "out": (out, F8, (B, n_sel, D)), "out_scale": (out_scale, torch.float32, (B, n_sel, _blocks(D)))},
+             (_ptr(x), _ptr(add), _ptr(idx), _ptr(shift), _ptr(scale), shift.stride(0) if B > 1 else D, _ptr(out), _ptr(out_scale),
+              B, N, n_sel, D, dtype))
+    return out, out_scale
+
+
+def _rms_tensors(name, x, add, gain, sum):
+    rows, D = _matrix(name, "x", x)
+    dtype = _run_dtype(name, x)
+    return rows, D, dtype, {"x": (x, x.dtype, (rows, D)), "add": (add, x.dtype, (rows, D)), "gain": (gain, x.dtype, (D,)),
+                            "sum": (sum, x.dtype, (rows, D))}
+
+
+def hero_rms_norm(x, add, gain, sum, out, eps: float = 1e-5):
+    """sum <- x + add, out <- (x + add) / sqrt(mean((x + add)^2) + eps) * gain over the rows of [rows, D]; add, gain and sum may be
+    None.  sum or out (not both) may be x or add."""
+    rows, D, dtype, tensors = _rms_tensors("hero_rms_norm", x, add, gain, sum)
+    tensors["out"] = (out, x.dtype, (rows, D))
+    _f8_call("hero_rms_norm", tensors, (_ptr(x), _ptr(add), _ptr(gain), _ptr(sum), _ptr(out), rows, D, eps, dtype))
+    return out
+
+
+def hero_rms_norm_fp8(x, add, gain, sum, out, out_scale, eps: float = 1e-5):
+    """hero_rms_norm with out in e4m3 (float8_e4m3fn [rows, D]) and a scale per row and 128 columns."""
+    rows, D, dtype, tensors = _rms_tensors("hero_rms_norm_fp8", x, add, gain, sum)
+    tensors["out"] = (out, F8, (rows, D))
+    tensors["out_scale"] = (out_scale, torch.float32, (rows, _blocks(D)))
+    _f8_call("hero_rms_norm_fp8", tensors,
+             (_ptr(x), _ptr(add), _ptr(gain), _ptr(sum), _ptr(out), _ptr(out_scale), rows, D, eps, dtype))
+    return out, out_scale
+
+
+def hero_gemm_fp8(a, a_scale, w, w_scale, bias, c, c_scale=None, act: int = 0):
+    """c <- act(A W^T + bias) of e4m3 operands a [M, K] (a_scale [M, ceil(K / 128)]) and w [N, K] (w_scale [ceil(N / 128),
+    ceil(K / 128)]); bias bf16 [N] or None, act 1: GELU-tanh.  c is bf16 or fp32 [M, N], or float8_e4m3fn with c_scale [M, ceil(N / 128)]."""
+    M, K = _matrix("hero_gemm_fp8", "a", a)
+    N = _matrix("hero_gemm_fp8", "w", w)[0]
+    _matrix("hero_gemm_fp8", "c", c)
+    out = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, F8: DTYPE_E4M3}.get(c.dtype)
+    if out is None:
+        raise HeroError(ERR_ARG, f"hero_gemm_fp8: c is bf16, fp32 or float8_e4m3fn, got {c.dtype}")
+    kb = _blocks(K)
+    _f8_call("hero_gemm_fp8",
+             {"a": (a, F8, (M, K)), "a_scale": (a_scale, torch.float32, (M, kb)), "w": (w, F8, (N, K)),
+              "w_scale": (w_scale, torch.float32, (_blocks(N), kb)), "bias": (bias, torch.bfloat16, (N,)), "c": (c, c.dtype, (M, N)),
+              "c_scale": (c_scale, torch.float32, (M, _blocks(N)))},
+             (_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(c), _ptr(c_scale), M, N, K, act, out))
+    return c
+
+
 # ---- what the rules on sizes choose (no GPU needed) --------------------------------
 def hero_plan_fp32_gemm(M: int, N: int, K: int, sms: int = 148):
     """(tile, thread blocks per tile) of a context's fp32 GEMM on a GPU of `sms` SMs."""
@@ -390,6 +515,13 @@ def hero_plan_bf16_gemm(M: int, N: int, K: int, qk: bool = False, sms: int = 148
     columns, ctas = C.c_int(), C.c_int()
     _check(load().hero_plan_bf16_gemm(M, N, K, int(qk), sms, C.byref(columns), C.byref(ctas)), "hero_plan_bf16_gemm")
     return columns.value, ctas.value
+
+
+def hero_plan_fp8_gemm(M: int, N: int, K: int, e4m3_out: bool = False, sms: int = 148):
+    """(columns of a tile, thread blocks that share its K, whether W and A have changed places) of the 8-bit GEMM."""
+    columns, ctas, swap = C.c_int(), C.c_int(), C.c_int()
+    _check(load().hero_plan_fp8_gemm(M, N, K, int(e4m3_out), sms, C.byref(columns), C.byref(ctas), C.byref(swap)), "hero_plan_fp8_gemm")
+    return columns.value, ctas.value, bool(swap.value)
 
 
 def hero_plan_fp32_attention(B: int, n_q: int, N: int, heads: int, head_dim: int, sms: int = 148):

@@ -938,6 +938,75 @@ int hero_gemm_bf16(const void* a, const void* w, const void* bias, void* cmat, i
   return launch_tc_gemm(a, w, bias, M, N, K, o, nullptr, st, (cudaStream_t)stream);
 }
 
+// ---------------------------------------------------------------- 8-bit operands with a scale for each block of 128
+static bool run_dtype(int dtype) { return dtype == HERO_DTYPE_FP32 || dtype == HERO_DTYPE_BF16; }
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int hero_quantize_fp8(const void* d_x, void* d_q, float* d_scale, int rows, int cols, int block_rows, int dtype, void* stream) {
+  if (rows < 0 || cols <= 0 || (block_rows != 1 && block_rows != 128) || !run_dtype(dtype)) return HERO_ERR_ARG;
+  if (cols % 16) return HERO_ERR_ALIGN;
+  if (rows == 0) return HERO_OK;
+  if (!d_x || !d_q || !d_scale) return HERO_ERR_ARG;
+  if (!aligned16(d_x) || !aligned16(d_q) || !aligned4(d_scale)) return HERO_ERR_ALIGN;
+  return launch_quantize_fp8(d_x, d_q, d_scale, rows, cols, block_rows, dtype, (cudaStream_t)stream);
+}
+
+int hero_gather_ln_modulate_fp8(const void* d_x, const void* d_add, const int* d_idx, const float* d_shift, const float* d_scale,
+                                int mod_ld, void* d_out, float* d_out_scale, int B, int N, int n_sel, int D, int dtype, void* stream) {
+  if (B < 0 || N < 0 || n_sel < 0 || n_sel > N || D <= 0 || mod_ld < D || !run_dtype(dtype)) return HERO_ERR_ARG;
+  if (D % 16) return HERO_ERR_ALIGN;
+  if (D > kMaxSmemFloats || (long long)B * n_sel > 0x7FFFFFFFll) return HERO_ERR_ARG;
+  if (B == 0 || n_sel == 0) return HERO_OK;
+  if (!d_x || !d_shift || !d_scale || !d_out || !d_out_scale) return HERO_ERR_ARG;
+  if (!aligned16(d_x) || !aligned16(d_out) || (d_add && !aligned16(d_add)) || !aligned4(d_idx) || !aligned4(d_shift) ||
+      !aligned4(d_scale) || !aligned4(d_out_scale))
+    return HERO_ERR_ALIGN;
+  return launch_gather_ln_modulate_fp8(d_x, d_add, d_idx, d_shift, d_scale, mod_ld, d_out, d_out_scale, B, N, n_sel, D, 1e-5f, dtype,
+                                       (cudaStream_t)stream);
+}
+
+static int check_rms_norm(const void* x, const void* add, const void* gain, const void* sum, const void* out, int rows, int D, float eps,
+                          int dtype) {
+  if (rows < 0 || D <= 0 || !(eps >= 0.f) || !run_dtype(dtype)) return HERO_ERR_ARG;
+  if (D % (dtype == HERO_DTYPE_BF16 ? 8 : 4)) return HERO_ERR_ALIGN;
+  if (D > kMaxSmemFloats) return HERO_ERR_ARG;
+  if (rows == 0) return HERO_OK;
+  if (!x || !out || sum == out) return HERO_ERR_ARG;
+  if (!aligned16(x) || !aligned16(add) || !aligned16(gain) || !aligned16(sum) || !aligned16(out)) return HERO_ERR_ALIGN;
+  return 1;
+}
+int hero_rms_norm(const void* d_x, const void* d_add, const void* d_gain, void* d_sum, void* d_out, int rows, int D, float eps, int dtype,
+                  void* stream) {
+  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, rows, D, eps, dtype);
+  if (r <= 0) return r;
+  return launch_rms_norm(d_x, d_add, d_gain, d_sum, d_out, nullptr, rows, D, eps, dtype, (cudaStream_t)stream);
+}
+int hero_rms_norm_fp8(const void* d_x, const void* d_add, const void* d_gain, void* d_sum, void* d_out, float* d_out_scale, int rows,
+                      int D, float eps, int dtype, void* stream) {
+  if (D > 0 && D % 16) return HERO_ERR_ALIGN;
+  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, rows, D, eps, dtype);
+  if (r <= 0) return r;
+  if (!d_out_scale || d_out == d_x || d_out == d_add) return HERO_ERR_ARG;
+  if (!aligned4(d_out_scale)) return HERO_ERR_ALIGN;
+  return launch_rms_norm(d_x, d_add, d_gain, d_sum, d_out, d_out_scale, rows, D, eps, dtype, (cudaStream_t)stream);
+}
+
+int hero_gemm_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const void* bias, void* cmat, float* c_scale,
+                  int M, int N, int K, int act, int out_dtype, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || (act != 0 && act != 1)) return HERO_ERR_ARG;
+  if (!run_dtype(out_dtype) && out_dtype != HERO_DTYPE_E4M3) return HERO_ERR_ARG;
+  const bool f8 = out_dtype == HERO_DTYPE_E4M3;
+  if (K % 16 || (f8 && N % 16)) return HERO_ERR_ALIGN;
+  if (M == 0) return HERO_OK;
+  if (!a || !a_scale || !w || !w_scale || !cmat || f8 != (c_scale != nullptr)) return HERO_ERR_ARG;
+  if (!aligned16(a) || !aligned16(w) || !aligned16(cmat) || !aligned4(a_scale) || !aligned4(w_scale) || !aligned4(c_scale) ||
+      (reinterpret_cast<uintptr_t>(bias) & 1u))
+    return HERO_ERR_ALIGN;
+  int* st = isolated_status();
+  if (!st) return HERO_ERR_NOMEM;
+  return launch_tc_gemm_fp8(a, a_scale, w, w_scale, bias, cmat, c_scale, M, N, K, act, out_dtype, st, (cudaStream_t)stream);
+}
+
 int hero_attention_bf16(const void* q, const void* k, const void* v, void* o, int B, int n_q, int N, int heads,
                         void* stream) {
   if (B < 0 || n_q < 0 || N <= 0 || heads <= 0) return HERO_ERR_ARG;
@@ -998,6 +1067,13 @@ int hero_plan_bf16_gemm(int M, int N, int K, int qk, int sms, int* columns, int*
   if (M <= 0 || N <= 0 || K <= 0 || (qk != 0 && qk != 1) || sms <= 0 || !columns || !ctas) return HERO_ERR_ARG;
   const TcGemmPlan plan = plan_tc_gemm(M, N, K, qk != 0, sms);
   *columns = plan.bn; *ctas = plan.split;
+  return HERO_OK;
+}
+
+int hero_plan_fp8_gemm(int M, int N, int K, int e4m3_out, int sms, int* columns, int* ctas, int* swap) {
+  if (M <= 0 || N <= 0 || K <= 0 || (e4m3_out != 0 && e4m3_out != 1) || sms <= 0 || !columns || !ctas || !swap) return HERO_ERR_ARG;
+  const TcGemmF8Plan plan = plan_tc_gemm_fp8(M, N, K, e4m3_out != 0, sms);
+  *columns = plan.bn; *ctas = plan.split; *swap = plan.swap;
   return HERO_OK;
 }
 

@@ -235,6 +235,17 @@ int launch_gather_ln_modulate(const void* x, const void* add, const int* idx, co
                               const float* scale, int mod_ld, void* a, int B, int N, int n_sel, int D,
                               float eps, int dtype, int settled, cudaStream_t s);
 
+// The same rows in e4m3 with a scale per 128 columns (a_scale [B, n_sel, ceil(D / 128)]).
+int launch_gather_ln_modulate_fp8(const void* x, const void* add, const int* idx, const float* shift, const float* scale,
+                                  int mod_ld, void* a, float* a_scale, int B, int N, int n_sel, int D, float eps, int dtype,
+                                  cudaStream_t s);
+// A matrix to e4m3 with a scale per block_rows x 128 elements (block_rows 1 or 128).
+int launch_quantize_fp8(const void* x, void* q, float* scale, int rows, int cols, int block_rows, int dtype, cudaStream_t s);
+// h = x + add, sum = h (either may be null), out = h / sqrt(mean(h^2) + eps) * gain (null: 1) in `dtype`, or, where out_scale is
+// given, in e4m3 with a scale per 128 columns.  At most 12288 columns.
+int launch_rms_norm(const void* x, const void* add, const void* gain, void* sum, void* out, float* out_scale, int rows, int D,
+                    float eps, int dtype, cudaStream_t s);
+
 // x = (x + ga) + gf for all rows and the LayerNorm + modulate of the rows that the next
 // block refreshes (pos: as SelectBatch::pos; null: all rows) into a [B, n_sel, D].  Rows as wide as residual_ln_serves.
 // Placed early, it reads all but gf before it waits for the kernel in front, which then has to be the only one on the stream
@@ -260,6 +271,12 @@ int plan_simt_attention(long long groups, int tiles, int head_dim, int sms);    
 int tc_init_driver_api();   // resolves cuTensorMapEncodeTiled once
 int launch_tc_gemm(const void* a, const void* w, const void* bias, int M, int Nout, int K,
                    const GemmOut& out, const QkEpilogue* qk, int* d_status, cudaStream_t s);
+// C = act(A W^T + bias) of e4m3 operands with block scales; out_dtype HERO_DTYPE_E4M3 writes c_scale as well.
+int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const void* bias, void* c,
+                       float* c_scale, int M, int Nout, int K, int act, int out_dtype, int* d_status, cudaStream_t s);
+// Columns of a tile and the CTAs that share its K (0: the kernel on CTA pairs); swap: tiles of 128 rows of W by bn rows of A.
+struct TcGemmF8Plan { int bn, split; bool swap; };
+TcGemmF8Plan plan_tc_gemm_fp8(int M, int Nout, int K, bool f8_out, int sms);
 // Columns of a tile and the CTAs that share its K (0: the kernel on CTA pairs).
 struct TcGemmPlan { int bn, split; };
 TcGemmPlan plan_tc_gemm(int M, int Nout, int K, bool qk, int sms);

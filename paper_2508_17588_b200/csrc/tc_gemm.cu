@@ -59,6 +59,21 @@ int make_tmap_bf16(CUtensorMap* m, const void* base, int rank, const uint64_t* d
   return HERO_OK;
 }
 
+// A byte matrix [rows, cols], rows contiguous; box = box_rows x 128 bytes, swizzle and fill as above.
+int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+  HERO_TRY(tc_init_driver_api());
+  const cuuint64_t gdim[2] = {cols, rows}, gstr[1] = {cols};
+  const cuuint32_t bx[2] = {128, box_rows}, es[2] = {1, 1};
+  CUresult r = g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstr, bx, es,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    return HERO_ERR_CUDA;
+  }
+  return HERO_OK;
+}
+
 namespace {
 using namespace tc;
 
@@ -67,18 +82,6 @@ constexpr int kABytes = kBM * kBK * 2;                 // 16 KB
 constexpr int kGemmThreads = 320;                      // producer, issuer, eight epilogue warps
 constexpr int kEpiWarps = 8;                           // two per TMEM lane quadrant, each with half of a tile's columns
 constexpr size_t kAlignSlack = 1024, kBarrierBytes = 512;
-
-__device__ __forceinline__ float gelu_tanh_f(float t) {
-  // 0.5 t (1 + tanh(sqrt(2/pi) (t + 0.044715 t^3))) with the hardware tanh (one special-function
-  // instruction, relative error 2^-11: below the bf16 rounding of the result).  The epilogue shares the
-  // SM's power budget with the tensor core, so every instruction saved here is tensor clock gained.
-  const float t2 = t * t;
-  const float u = t * fmaf(0.0356774081f, t2, 0.7978845608f);
-  float th;
-  asm("tanh.approx.f32 %0, %1;" : "=f"(th) : "f"(u));
-  const float h = 0.5f * t;
-  return fmaf(h, th, h);
-}
 
 // Where one accumulator row goes.
 struct RowOut {
@@ -290,21 +293,6 @@ struct PairCfg {
   static constexpr size_t kBiasBytes = kEpiWarps * 2 * (BN / 2) * 4;   // a warp's columns of two tiles
   static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kBarrierBytes;
 };
-
-// Tile order of the persistent pairs.  Consecutive tile numbers run down kGroupM row tiles (of 256) before moving to
-// the next column tile, and only then to the next band of rows: the 74 tiles in flight at any time then cover about
-// 12 x 6 tiles, whose operands stay in L2 and are shared by the pairs working on them, instead of every pair
-// streaming its own panel of A from DRAM.
-constexpr int kGroupM = 12;
-__device__ __forceinline__ void tile_coords(int tile, int m_tiles, int n_tiles, int& mt, int& nt) {
-  const int per_group = kGroupM * n_tiles;
-  const int group = tile / per_group;
-  const int first_m = group * kGroupM;
-  const int rows = min(kGroupM, m_tiles - first_m);
-  const int r = tile - group * per_group;
-  mt = first_m + r % rows;
-  nt = r / rows;
-}
 
 template <int BN, bool QK>
 __global__ void __launch_bounds__(kGemmThreads, 1)

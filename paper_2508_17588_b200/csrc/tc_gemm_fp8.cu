@@ -1,0 +1,706 @@
+// 8-bit GEMM on the 5th-generation tensor cores, operands in e4m3 with a scale for each block of 128:
+//   C[m, n] = act( sum_kb sA[m, kb] * sW[n / 128, kb] * (sum over the 128 columns of kb of A[m, k] W[n, k]) + bias[n] )
+// with kb the blocks of 128 columns.  A has a scale per row and block, W one per 128 x 128 elements.
+//
+// The scales are any fp32 numbers, so a block's sum cannot simply go on in the tensor core's accumulator: the MMAs of one block
+// (four steps of K = 32, one 128-byte swizzle row) write a TMEM buffer of their own, and the epilogue warps take it into fp32
+// registers with one packed FMA per two sums, acc += (sA sW) * sum, while the MMAs of the next block fill the other buffer.  A
+// scale is a block's maximum / 448, so what is summed inside a block is bounded by 128 * 448^2 and the sum over the blocks runs
+// in fp32 registers, in the order of the blocks.
+//
+// Two kernels (launch_tc_gemm_fp8 says which runs when):
+//  * fp8_pair_kernel for problems that fill the chip: persistent CTA pairs on 256-row tiles (cta_group::2);
+//  * fp8_split_kernel for the others: one tile per CTA, the K loop cut over the CTAs of a cluster; with few rows of A the roles of
+//    the operands are exchanged, so that a tile is 128 rows of W by 16, 32 or 64 rows of A.
+#include <cuda.h>
+
+#include "fp8_common.cuh"
+#include "hero_internal.h"
+#include "tc_common.cuh"
+
+namespace hero {
+
+int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+
+namespace {
+using namespace tc;
+
+constexpr int kRows = 128;                       // rows of a tile (of the first operand) per CTA
+constexpr int kStepK = kF8Block;                 // a K step is a block of scales: 128 bytes of a row
+constexpr int kRowBytes = kRows * kStepK;        // 16 KB
+constexpr size_t kAlignSlack = 1024, kBarrierBytes = 512;
+
+enum { kOutF32 = HERO_DTYPE_FP32, kOutBf16 = HERO_DTYPE_BF16, kOutF8 = HERO_DTYPE_E4M3 };
+
+// Everything about the operands' scales and the result that a kernel needs.
+struct F8Gemm {
+  const float* a_scale;          // [M, kb]
+  const float* w_scale;          // [ceil(N / 128), kb]
+  const __nv_bfloat16* bias;     // [N] or null
+  void* c;                       // [M, N]
+  float* c_scale;                // [M, ceil(N / 128)], for e4m3 results
+  int M, N, K, act;
+  int vec;                       // rows of C start on multiples of: 32, 16 or 0 (less) bytes
+};
+
+// GELU-tanh to fp32 accuracy: t (1 + tanh u) / 2 = t / (1 + exp(-2u)).  (bf16 results take the hardware tanh, which is
+// exact enough for their rounding and one special-function instruction less.)
+__device__ __forceinline__ float gelu_exact_f(float t) {
+  const float u = t * fmaf(0.0356774081f, t * t, 0.7978845608f);
+  return __fdividef(t, 1.0f + __expf(-2.0f * u));
+}
+template <int OUT>
+__device__ __forceinline__ float gelu(float t) { return OUT == kOutBf16 ? gelu_tanh_f(t) : gelu_exact_f(t); }
+
+// Wait for 16 columns asked for with tmem_ld16; the registers are named so that nothing that uses them moves ahead of it.
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+// acc += s * (NC columns of this thread's TMEM lane), 16 columns on their way while 16 are added.
+template <int NC>
+__device__ __forceinline__ void promote(float2 (&acc)[NC / 2], uint32_t taddr, float s) {
+  uint32_t r[2][16];
+  const float2 s2 = make_float2(s, s);
+  tmem_ld16(taddr, r[0]);
+#pragma unroll
+  for (int c = 0; c < NC / 16; ++c) {
+    tmem_wait16(r[c & 1]);
+    if (c + 1 < NC / 16) tmem_ld16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      acc[c * 8 + i] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), s2, acc[c * 8 + i]);
+  }
+}
+// The same with a factor per column: that of column c is lane c's `s` (columns 32 and on: lane c - 32's `s_hi`).
+template <int NC>
+__device__ __forceinline__ void promote_columns(float2 (&acc)[NC / 2], uint32_t taddr, float s, float s_hi) {
+  uint32_t r[2][16];
+  tmem_ld16(taddr, r[0]);
+#pragma unroll
+  for (int c = 0; c < NC / 16; ++c) {
+    float2 f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int col = c * 16 + 2 * i;
+      const float from = col < 32 ? s : s_hi;
+      f[i] = make_float2(__shfl_sync(0xFFFFFFFFu, from, col & 31), __shfl_sync(0xFFFFFFFFu, from, (col + 1) & 31));
+    }
+    tmem_wait16(r[c & 1]);
+    if (c + 1 < NC / 16) tmem_ld16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      acc[c * 8 + i] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), f[i], acc[c * 8 + i]);
+  }
+}
+
+// A warp puts NC bias values from column n0 on into its own piece of shared memory, in fp32; zeros past the end of the row and
+// where there is no bias.
+template <int NC>
+__device__ __forceinline__ void stage_bias(float* s_bias, const __nv_bfloat16* bias, int n0, int N, int lane) {
+  __syncwarp();                              // (all lanes are done with what is there)
+#pragma unroll
+  for (int i = lane; i < NC; i += 32) s_bias[i] = bias != nullptr && n0 + i < N ? __bfloat162float(__ldg(bias + n0 + i)) : 0.f;
+  __syncwarp();
+}
+
+// One row's NC columns: bias and activation.
+template <int NC, int OUT>
+__device__ __forceinline__ void finish_row(float2 (&acc)[NC / 2], const float* s_bias, int act) {
+#pragma unroll
+  for (int v = 0; v < NC / 4; ++v) {
+    const float4 b4 = *reinterpret_cast<const float4*>(s_bias + v * 4);
+    acc[2 * v] = __fadd2_rn(acc[2 * v], make_float2(b4.x, b4.y));
+    acc[2 * v + 1] = __fadd2_rn(acc[2 * v + 1], make_float2(b4.z, b4.w));
+  }
+  if (act) {
+#pragma unroll
+    for (int i = 0; i < NC / 2; ++i) acc[i] = make_float2(gelu<OUT>(acc[i].x), gelu<OUT>(acc[i].y));
+  }
+}
+template <int NC>
+__device__ __forceinline__ uint32_t row_amax(const float2 (&acc)[NC / 2]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < NC / 2; ++i) m = max(m, max(abs_bits(acc[i].x), abs_bits(acc[i].y)));
+  return m;
+}
+__device__ __forceinline__ uint32_t bf16x2(float2 f) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+// 32 bytes of a row of `size`-byte elements from column n on, as far as the row goes.
+template <typename T>
+__device__ __forceinline__ void store32(T* dst, const uint32_t (&w)[8], int n, int N, int vec) {
+  constexpr int kPer = 32 / (int)sizeof(T);
+  if (vec == 32) {
+    if (n < N) st_global_v8(dst, w);
+  } else if (vec == 16) {
+    if (n < N) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (n + kPer / 2 < N) *reinterpret_cast<uint4*>(dst + kPer / 2) = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (n + i < N) {
+        constexpr int kIn = 4 / (int)sizeof(T);
+        const uint32_t word = w[i / kIn] >> (8 * sizeof(T) * (i % kIn));
+        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[i] = word;
+        else if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)word;
+        else reinterpret_cast<uint8_t*>(dst)[i] = (uint8_t)word;
+      }
+  }
+}
+template <int NC, int OUT>
+__device__ __forceinline__ void store_row(const float2 (&acc)[NC / 2], const F8Gemm& g, int m, int n0, float inv) {
+  if constexpr (OUT == kOutF32) {
+    float* dst = static_cast<float*>(g.c) + (long long)m * g.N + n0;
+#pragma unroll
+    for (int v = 0; v < NC / 8; ++v) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { w[2 * i] = __float_as_uint(acc[4 * v + i].x); w[2 * i + 1] = __float_as_uint(acc[4 * v + i].y); }
+      store32(dst + v * 8, w, n0 + v * 8, g.N, g.vec);
+    }
+  } else if constexpr (OUT == kOutBf16) {
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(g.c) + (long long)m * g.N + n0;
+#pragma unroll
+    for (int v = 0; v < NC / 16; ++v) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = bf16x2(acc[8 * v + i]);
+      store32(dst + v * 16, w, n0 + v * 16, g.N, g.vec);
+    }
+  } else {
+    uint8_t* dst = static_cast<uint8_t*>(g.c) + (long long)m * g.N + n0;
+#pragma unroll
+    for (int v = 0; v < NC / 32; ++v) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 a = acc[16 * v + 2 * i], b = acc[16 * v + 2 * i + 1];
+        w[i] = f8_pack4(a.x * inv, a.y * inv, b.x * inv, b.y * inv);
+      }
+      store32(dst + v * 32, w, n0 + v * 32, g.N, g.vec);
+    }
+  }
+}
+// Finish and store NC columns of a row.  e4m3: the two warps of a TMEM quadrant that hold halves of a block trade their maxima
+// through `s_amax` (two words a row); NC = 128 is a block by itself.
+template <int NC, int OUT>
+__device__ __forceinline__ void emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, uint32_t* s_amax,
+                                         int tile_row, int half, int quad) {
+  finish_row<NC, OUT>(acc, s_bias, g.act);
+  float inv = 0.f;
+  if constexpr (OUT == kOutF8) {
+    uint32_t amax = row_amax<NC>(acc);
+    if constexpr (NC < kF8Block) {
+      static_assert(2 * NC == kF8Block, "two warps hold a block");
+      s_amax[2 * tile_row + half] = amax;
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
+      amax = max(amax, s_amax[2 * tile_row + (half ^ 1)]);
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");      // (the words are free for the next tile)
+    }
+    const F8Scale s = f8_scale(amax);
+    inv = s.inv;
+    if (m < g.M && n0 < g.N && n0 % kF8Block == 0) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
+  }
+  if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// One tile per CTA.  A tile is 128 rows of the first operand by BN of the second: of A by W, or (SWAP) of W by A, for
+// few rows of A.  A cluster of `split` CTAs shares a tile, each taking a run of its K blocks; their partial sums meet through
+// distributed shared memory, added in rank order.
+//   warp 0     TMA producer
+//   warp 1     MMA issuer
+//   warps 2..  promotion and epilogue: eight (two per TMEM quadrant, half of the columns each), SWAP: four
+// ---------------------------------------------------------------------------------------------------------------
+template <int BN, bool SWAP>
+struct SplitCfg {
+  static constexpr int kWarps = SWAP ? 4 : 8;
+  static constexpr int kThreads = 64 + 32 * kWarps;
+  static constexpr int kCols = SWAP ? BN : BN / 2;             // of a warp
+  static constexpr int kStageBytes = kRowBytes + BN * kStepK;
+  static constexpr int kStages = !SWAP ? (BN == 128 ? 4 : 6) : (BN == 16 ? 5 : (BN == 32 ? 4 : 3));
+  static constexpr int kTmemCols = 2 * BN;                     // (a power of two, at least 32)
+  static constexpr int kMaxSplit = SWAP ? 8 : 4;
+  static constexpr size_t kBiasBytes = SWAP ? 0 : (size_t)kWarps * kCols * 4;
+  static constexpr size_t kAmaxBytes = SWAP ? (size_t)4 * BN * 4 : (size_t)2 * kRows * 4;
+  static constexpr size_t part_bytes(int split) {              // columns of A's rows, or 128 / split rows, from each of the others
+    return SWAP ? (size_t)(split - 1) * (BN / split) * kRows * 4 : (size_t)(split - 1) * (kRows / split) * BN * 4;
+  }
+  static constexpr size_t smem(int split) {
+    return kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kAmaxBytes + kBarrierBytes + part_bytes(split);
+  }
+};
+
+template <int BN, bool SWAP, int OUT>
+__global__ void __launch_bounds__(SplitCfg<BN, SWAP>::kThreads)
+fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const F8Gemm g, int split,
+                 int* __restrict__ status) {
+  using Cfg = SplitCfg<BN, SWAP>;
+  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
+  uint32_t* s_amax = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_amax) + Cfg::kAmaxBytes);
+  uint64_t* full = bars;                    // [kStages] TMA -> MMA
+  uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA
+  uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion
+  uint64_t* acc_empty = acc_full + 2;       // [2] promotion -> MMA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* s_part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kBarrierBytes);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = split > 1 ? (int)cluster_rank() : 0;
+  const int tile = blockIdx.x / split;
+  const int m_tile = SWAP ? BN : kRows, n_tile = SWAP ? kRows : BN;
+  const int m_tiles = (g.M - 1) / m_tile + 1;
+  const int m0 = (tile % m_tiles) * m_tile, n0 = (tile / m_tiles) * n_tile;
+  const int k_blocks = (g.K - 1) / kStepK + 1;
+  const int kb0 = (int)((long long)k_blocks * rank / split), kb1 = (int)((long long)k_blocks * (rank + 1) / split);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kWarps); }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 0 && lane == 0) { tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_w); }
+  if (warp == 1) { tmem_alloc(tmem_slot, Cfg::kTmemCols); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (split > 1) cluster_arrive();           // waited for before anything is sent to another CTA
+  const uint32_t tmem_base = *tmem_slot;
+  stream_order();
+
+  float2 acc[kCols / 2];
+  bool ok = true;
+  const int quad = warp & 3;                 // TMEM lane quadrant this warp may read
+  const int half = SWAP ? 0 : (warp - 2) >> 2;
+  const int tile_row = quad * 32 + lane;
+  float* s_bias = s_bias_all + (SWAP || warp < 2 ? 0 : (size_t)(warp - 2) * kCols);
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int stage = 0; uint32_t phase = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        uint8_t* first = smem + (size_t)stage * Cfg::kStageBytes;
+        uint8_t* second = first + kRowBytes;
+        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
+        mbar_expect_tx(&full[stage], Cfg::kStageBytes);
+        tma_load_2d(SWAP ? first : second, &tm_w, &full[stage], kb * kStepK, n0);
+        tma_load_2d(SWAP ? second : first, &tm_a, &full[stage], kb * kStepK, m0);
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+      for (int i = 0; i < kStages; ++i) {      // all armed stages consumed before the CTA retires
+        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    const bool leader = elect_one();
+    constexpr uint32_t idesc = idesc_e4m3(kRows, BN);
+    int stage = 0; uint32_t phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const int j = kb - kb0, buf = j & 1;
+      if (!mbar_wait_warp(&acc_empty[buf], ((j >> 1) & 1) ^ 1, abort_flag)) break;
+      if (!mbar_wait_warp(&full[stage], phase, abort_flag)) break;
+      tc_fence_after();
+      const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes);
+      const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes, 1024);
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < kStepK / 32; ++k)   // +32 bytes (encoded >>4) per K step of 32 inside the swizzle atom
+          mma_f8_ss(tmem_base + buf * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
+        mma_commit(&empty[stage]);
+        mma_commit(&acc_full[buf]);
+      }
+      if (++stage == kStages) { stage = 0; phase ^= 1; }
+    }
+  } else {
+    // ------------------------------------------------------------ promotion
+    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
+    if constexpr (!SWAP) stage_bias<kCols>(s_bias, g.bias, n0 + half * kCols, g.N, lane);
+#pragma unroll
+    for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
+    // Scales are fetched a block ahead.  Rows and blocks past the end take the last one's (what they scale is not stored).
+    const float* sw = g.w_scale + (long long)(n0 / kF8Block) * k_blocks;
+    const int row = SWAP ? min(m0 + lane, g.M - 1) : min(m0 + tile_row, g.M - 1);
+    const float* sa = g.a_scale + (long long)row * k_blocks;
+    const float* sa_hi = g.a_scale + (long long)min(m0 + 32 + lane, g.M - 1) * k_blocks;      // SWAP, rows 32 and on
+    float f = 0.f, f_hi = 0.f;
+    if (kb0 < kb1) {
+      f = __ldg(sa + kb0) * __ldg(sw + kb0);
+      if (SWAP && BN > 32) f_hi = __ldg(sa_hi + kb0) * __ldg(sw + kb0);
+    }
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const int j = kb - kb0, buf = j & 1, ahead = min(kb + 1, kb1 - 1);
+      const float w_next = __ldg(sw + ahead), a_next = __ldg(sa + ahead);
+      float hi_next = 0.f;
+      if (SWAP && BN > 32) hi_next = __ldg(sa_hi + ahead);
+      if (!(ok = mbar_wait_warp(&acc_full[buf], (j >> 1) & 1, abort_flag))) break;
+      tc_fence_after();
+      if constexpr (SWAP) promote_columns<kCols>(acc, t_row + buf * BN, f, f_hi);
+      else promote<kCols>(acc, t_row + buf * BN, f);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      f = a_next * w_next;
+      f_hi = hi_next * w_next;
+    }
+  }
+
+  // ---------------------------------------------------------------- partial sums
+  // A CTA finishes 128 / split rows (whole TMEM quadrants), or (SWAP) every split-th column.
+  const int shift = split == 8 ? 3 : (split == 4 ? 2 : (split == 2 ? 1 : 0));
+  const int owner = (quad << shift) >> 2;
+  const int rows_own = kRows >> shift, own_row = tile_row - owner * rows_own;
+  const int columns = SWAP ? min(BN, g.M - m0) : BN;           // that exist
+  if (split > 1) {
+    __syncwarp();
+    cluster_wait();                          // the other CTAs have started (long since)
+    if (warp >= 2 && ok) {
+      if constexpr (SWAP) {
+#pragma unroll
+        for (int c = 0; c < BN; ++c) {
+          const int to = c & (split - 1);
+          if (c < columns && to != rank) {   // (warp-uniform)
+            const int slot = rank < to ? rank : rank - 1;
+            const float v = c & 1 ? acc[c / 2].y : acc[c / 2].x;
+            st_cluster_f32(cluster_map(smem_u32(s_part + ((size_t)slot * (BN >> shift) + (c >> shift)) * kRows + tile_row), (uint32_t)to), v);
+          }
+        }
+      } else if (owner != rank) {
+        const int slot = rank < owner ? rank : rank - 1;
+        const uint32_t base = cluster_map(smem_u32(s_part + (((size_t)slot * (BN / 4) + half * (kCols / 4)) * rows_own + own_row) * 4), (uint32_t)owner);
+#pragma unroll
+        for (int v = 0; v < kCols / 4; ++v)
+          st_cluster_v4(base + v * rows_own * 16, acc[2 * v].x, acc[2 * v].y, acc[2 * v + 1].x, acc[2 * v + 1].y);
+      }
+    }
+    __syncwarp();
+    cluster_sync();                          // every wait above is bounded, so everybody gets here
+    if (warp >= 2 && ok) {
+      for (int s = 0; s < split - 1; ++s) {
+        if constexpr (SWAP) {
+#pragma unroll
+          for (int c = 0; c < BN; ++c)
+            if (c < columns && (c & (split - 1)) == rank) {
+              const float v = s_part[((size_t)s * (BN >> shift) + (c >> shift)) * kRows + tile_row];
+              if (c & 1) acc[c / 2].y += v; else acc[c / 2].x += v;
+            }
+        } else if (owner == rank) {
+          const float4* part = reinterpret_cast<const float4*>(s_part) + ((size_t)s * (BN / 4) + half * (kCols / 4)) * rows_own + own_row;
+#pragma unroll
+          for (int v = 0; v < kCols / 4; ++v) {
+            const float4 p = part[v * rows_own];
+            acc[2 * v].x += p.x; acc[2 * v].y += p.y; acc[2 * v + 1].x += p.z; acc[2 * v + 1].y += p.w;
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- epilogue
+  if (warp >= 2) {
+    if constexpr (!SWAP) {
+      // (e4m3: the two warps of a quadrant meet in emit_row, so they enter it whatever became of their waits; a row that does
+      // not exist is not stored)
+      if (owner == rank)
+        emit_row<kCols, OUT>(acc, g, s_bias, ok ? m0 + tile_row : g.M, n0 + half * kCols, s_amax, tile_row, half, quad);
+    } else {
+      const int n = n0 + tile_row;
+      const float b = g.bias != nullptr && n < g.N ? __bfloat162float(__ldg(g.bias + n)) : 0.f;
+#pragma unroll
+      for (int c = 0; c < BN; ++c) {
+        float& v = c & 1 ? acc[c / 2].y : acc[c / 2].x;
+        v += b;
+        if (g.act) v = gelu<OUT>(v);
+      }
+      F8Scale sc = {};
+      if constexpr (OUT == kOutF8) {         // the 128 rows of W are a block: a column's maximum over the four warps
+#pragma unroll
+        for (int c = 0; c < BN; ++c) {
+          const uint32_t amax = __reduce_max_sync(0xFFFFFFFFu, abs_bits(c & 1 ? acc[c / 2].y : acc[c / 2].x));
+          if (lane == 0) s_amax[quad * BN + c] = amax;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+      }
+#pragma unroll
+      for (int c = 0; c < BN; ++c) {
+        if (ok && c < columns && (c & (split - 1)) == rank) {  // (warp-uniform)
+          const float v = c & 1 ? acc[c / 2].y : acc[c / 2].x;
+          const long long at = (long long)(m0 + c) * g.N + n;
+          if constexpr (OUT == kOutF8) {
+            sc = f8_scale(max(max(s_amax[c], s_amax[BN + c]), max(s_amax[2 * BN + c], s_amax[3 * BN + c])));
+            if (n < g.N) static_cast<uint8_t*>(g.c)[at] = (uint8_t)f8_pack4(v * sc.inv, 0.f, 0.f, 0.f);
+            if (tile_row == 0) g.c_scale[(long long)(m0 + c) * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = sc.scale;
+          } else if (n < g.N) {
+            if constexpr (OUT == kOutBf16) static_cast<__nv_bfloat16*>(g.c)[at] = __float2bfloat16_rn(v);
+            else static_cast<float*>(g.c)[at] = v;
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(status, 1);
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, Cfg::kTmemCols); }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Persistent clusters of two CTAs, one per pair of SMs, on tiles of 256 x BN: each CTA fetches its own 128 rows of A and half
+// of the tile's rows of W, a K step of 128 costs an SM 32 KB from L2 (BN = 256) for the 8.4 MFLOP it computes.
+//   warp 0      TMA producer (both CTAs, each its own operand rows; all bytes reported to the even CTA's barrier)
+//   warp 1      MMA issuer (even CTA only): 4 x tcgen05.mma M256 N=BN K32 per block into one of two TMEM buffers; the commits
+//               free both CTAs' stage and hand the buffer to both CTAs' promotion
+//   warps 2..9  promotion and epilogue (both CTAs, each its own 128 rows; two warps share 32 rows, half of the columns each)
+// ---------------------------------------------------------------------------------------------------------------
+template <int BN>
+struct PairCfg {
+  static constexpr int kWarps = 8, kThreads = 320, kCols = BN / 2;
+  static constexpr int kStageBytes = kRowBytes + BN / 2 * kStepK;
+  static constexpr int kStages = 196608 / kStageBytes;         // 192 KB: 6 (BN = 256) or 8 (BN = 128)
+  static constexpr int kTmemCols = 2 * BN;
+  static constexpr size_t kBiasBytes = (size_t)kWarps * kCols * 4;
+  static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kBarrierBytes;
+};
+
+template <int BN, int OUT>
+__global__ void __launch_bounds__(PairCfg<BN>::kThreads, 1)
+fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const F8Gemm g,
+                int* __restrict__ status) {
+  static_assert(OUT != kOutF8 || BN == 256, "a thread holds a whole block of an e4m3 result");
+  using Cfg = PairCfg<BN>;
+  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols;
+  extern __shared__ uint8_t smem_raw[];
+  // The dynamic shared memory starts at the same offset in both CTAs, and so does everything carved from it: a
+  // descriptor or a barrier offset means the same place in either.
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
+  uint64_t* full = bars;                    // [kStages] both CTAs' TMA -> MMA (the even CTA's is the one in use)
+  uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA (each CTA its own)
+  uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion (each CTA its own)
+  uint64_t* acc_empty = acc_full + 2;       // [2] both CTAs' promotion -> MMA (the even CTA's)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int m_tiles = (g.M - 1) / (2 * kRows) + 1, n_tiles = (g.N - 1) / BN + 1;
+  const int n_tiles_total = m_tiles * n_tiles;
+  const int k_blocks = (g.K - 1) / kStepK + 1;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * Cfg::kWarps); }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 0 && lane == 0) { tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_w); }
+  if (warp == 1) tmem_alloc_pair(tmem_slot, Cfg::kTmemCols);
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync();                           // both CTAs' barriers exist before anybody signals across
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  stream_order();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int stage = 0; uint32_t phase = 0;
+      bool ok = true;
+      for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
+        int mt, nt;
+        tile_coords(tile, m_tiles, n_tiles, mt, nt);
+        const int row_a = (2 * mt + (int)rank) * kRows, row_w = nt * BN + (int)rank * (BN / 2);
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!(ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag))) break;
+          // The even CTA's barrier counts the bytes of both CTAs.  The odd CTA's may land before it is armed: its
+          // phase cannot complete before the arrival that arms it.
+          if (rank == 0) mbar_expect_tx(&full[stage], 2 * Cfg::kStageBytes);
+          const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes), bar = cluster_map(smem_u32(&full[stage]), 0);
+          tma_load_2d_pair(sa, &tm_a, bar, kb * kStepK, row_a);
+          tma_load_2d_pair(sa + kRowBytes, &tm_w, bar, kb * kStepK, row_w);
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+      // On the way out make sure every stage that was armed has been consumed (bounded): the CTA must
+      // not retire with bulk copies still writing its shared memory.
+      for (int i = 0; i < kStages; ++i) {
+        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (even CTA)
+    if (rank == 0) {
+      const bool leader = elect_one();
+      constexpr uint32_t idesc = idesc_e4m3(2 * kRows, BN);
+      int stage = 0; uint32_t phase = 0;
+      bool ok = true;
+      uint32_t j = 0;                        // K blocks so far
+      for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
+        for (int kb = 0; kb < k_blocks; ++kb, ++j) {
+          const uint32_t buf = j & 1;
+          if (!(ok = mbar_wait_warp(&acc_empty[buf], ((j >> 1) & 1) ^ 1, abort_flag))) break;
+          if (!(ok = mbar_wait_warp(&full[stage], phase, abort_flag))) break;
+          tc_fence_after();
+          const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes);
+          const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes, 1024);
+          if (leader) {
+#pragma unroll
+            for (int k = 0; k < kStepK / 32; ++k)
+              mma_f8_ss_pair(tmem_base + buf * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
+            mma_commit_pair(&empty[stage]);
+            mma_commit_pair(&acc_full[buf]);
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ promotion and epilogue (warps 2..9)
+    const int quad = warp & 3;                 // TMEM lane quadrant this warp may read
+    const int half = (warp - 2) >> 2;          // which half of the tile's columns it has
+    float* s_bias = s_bias_all + (size_t)(warp - 2) * kCols;
+    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
+    bool ok = true;
+    uint32_t j = 0;
+    for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
+      int mt, nt;
+      tile_coords(tile, m_tiles, n_tiles, mt, nt);
+      const int m = (2 * mt + (int)rank) * kRows + quad * 32 + lane, n_first = nt * BN + half * kCols;
+      stage_bias<kCols>(s_bias, g.bias, n_first, g.N, lane);
+      // Scales are fetched a block ahead.  Rows and blocks past the end take the last one's (what they scale is not stored).
+      const float* sw = g.w_scale + (long long)(min(n_first, g.N - 1) / kF8Block) * k_blocks;
+      const float* sa = g.a_scale + (long long)min(m, g.M - 1) * k_blocks;
+      float f = __ldg(sa) * __ldg(sw);
+      float2 acc[kCols / 2];
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
+      for (int kb = 0; kb < k_blocks; ++kb, ++j) {
+        const uint32_t buf = j & 1;
+        const int ahead = min(kb + 1, k_blocks - 1);
+        const float a_next = __ldg(sa + ahead), w_next = __ldg(sw + ahead);
+        if (!(ok = mbar_wait_warp(&acc_full[buf], (j >> 1) & 1, abort_flag))) break;
+        tc_fence_after();
+        promote<kCols>(acc, t_row + buf * BN, f);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_map(smem_u32(&acc_empty[buf]), 0));
+        f = a_next * w_next;
+      }
+      if (ok) emit_row<kCols, OUT>(acc, g, s_bias, m, n_first, nullptr, 0, half, quad);
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync();                            // neither CTA leaves while the other may still reach into it
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(status, 1);
+  if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, Cfg::kTmemCols); }
+}
+
+template <int BN, int OUT>
+int launch_pair(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
+  static PerDeviceOnce attr_once;            // the opt-in is a property of the kernel ON a device
+  HERO_TRY(per_device_once(attr_once, [](int) {
+    HERO_CUDA_TRY(cudaFuncSetAttribute(fp8_pair_kernel<BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg<BN>::kSmem));
+    return HERO_OK;
+  }));
+  const long long tiles = (long long)((g.M - 1) / (2 * kRows) + 1) * ((g.N - 1) / BN + 1);
+  if (tiles > 0x3FFFFFFF) return HERO_ERR_ARG;
+  const int pairs = tiles < num_sms() / 2 ? (int)tiles : num_sms() / 2;
+  return launch_kernel(fp8_pair_kernel<BN, OUT>, (unsigned)(2 * pairs), PairCfg<BN>::kThreads, PairCfg<BN>::kSmem, s, 2, tm_a, tm_w, g,
+                       d_status);
+}
+
+template <int BN, bool SWAP, int OUT>
+int launch_split(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int split, int* d_status, cudaStream_t s) {
+  using Cfg = SplitCfg<BN, SWAP>;
+  static PerDeviceOnce attr_once;
+  HERO_TRY(per_device_once(attr_once, [](int) {
+    HERO_CUDA_TRY(cudaFuncSetAttribute(fp8_split_kernel<BN, SWAP, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)Cfg::smem(Cfg::kMaxSplit)));
+    return HERO_OK;
+  }));
+  const int m_tile = SWAP ? BN : kRows, n_tile = SWAP ? kRows : BN;
+  const long long ctas = (long long)((g.M - 1) / m_tile + 1) * ((g.N - 1) / n_tile + 1) * split;
+  if (ctas > 0x7FFFFFFF) return HERO_ERR_ARG;
+  return launch_kernel(fp8_split_kernel<BN, SWAP, OUT>, (unsigned)ctas, Cfg::kThreads, Cfg::smem(split), s, (unsigned)split, tm_a, tm_w,
+                       g, split, d_status);
+}
+
+template <int OUT>
+int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
+  if (plan.split == 0) {
+    if constexpr (OUT != kOutF8)
+      if (plan.bn == 128) return launch_pair<128, OUT>(tm_a, tm_w, g, d_status, s);
+    return launch_pair<256, OUT>(tm_a, tm_w, g, d_status, s);
+  }
+  if (plan.swap) {
+    switch (plan.bn) {
+      case 16: return launch_split<16, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
+      case 32: return launch_split<32, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
+      default: return launch_split<64, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
+    }
+  }
+  if constexpr (OUT != kOutF8)
+    if (plan.bn == 64) return launch_split<64, false, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
+  return launch_split<128, false, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
+}
+
+}  // namespace
+
+TcGemmF8Plan plan_tc_gemm_fp8(int M, int Nout, int K, bool f8_out, int sms) {
+  const long long kb = ((long long)K + kStepK - 1) / kStepK;
+  auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
+  auto spread = [&](long long tiles, long long room, int most) {
+    int split = 1;
+    while (split * 2 <= most && split * 2 <= kb && tiles * split * 2 <= room) split *= 2;
+    return split;
+  };
+  if (M <= 64) {
+    const int bn = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
+    return {bn, spread(ceil_div(Nout, kRows), 2 * sms, 8), true};
+  }
+  if (ceil_div(M, 256) * ceil_div(Nout, 256) >= 60) return {256, 0, false};
+  const long long tiles = ceil_div(M, kRows) * ceil_div(Nout, 128);
+  return {128, spread(tiles, sms, 4), false};
+}
+
+int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const void* bias, void* c,
+                       float* c_scale, int M, int Nout, int K, int act, int out_dtype, int* d_status, cudaStream_t s) {
+  const TcGemmF8Plan plan = plan_tc_gemm_fp8(M, Nout, K, out_dtype == HERO_DTYPE_E4M3, num_sms());
+  CUtensorMap tm_a, tm_w;
+  HERO_TRY(make_tmap_bytes(&tm_a, a, (uint64_t)M, (uint64_t)K, plan.swap ? plan.bn : kRows));
+  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? plan.bn / 2 : (plan.swap ? kRows : plan.bn)));
+  F8Gemm g = {a_scale, w_scale, static_cast<const __nv_bfloat16*>(bias), c, c_scale, M, Nout, K, act, 0};
+  const unsigned long long low = (unsigned long long)reinterpret_cast<uintptr_t>(c) |
+                                 (unsigned long long)Nout * (out_dtype == HERO_DTYPE_FP32 ? 4 : (out_dtype == HERO_DTYPE_BF16 ? 2 : 1));
+  g.vec = low % 32 == 0 ? 32 : (low % 16 == 0 ? 16 : 0);
+  switch (out_dtype) {
+    case HERO_DTYPE_FP32: return launch_out<kOutF32>(plan, tm_a, tm_w, g, d_status, s);
+    case HERO_DTYPE_BF16: return launch_out<kOutBf16>(plan, tm_a, tm_w, g, d_status, s);
+    default: return launch_out<kOutF8>(plan, tm_a, tm_w, g, d_status, s);
+  }
+}
+
+}  // namespace hero
