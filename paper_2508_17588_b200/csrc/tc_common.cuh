@@ -97,6 +97,27 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
   return mbar_wait_warp_more(bar, parity, abort_flag, budget_ns);
 }
 
+// The same wait without a function call, for code whose registers a call would push out (a warp that holds 128 sums a thread).
+__device__ __forceinline__ bool mbar_wait_warp_inline(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  __syncwarp();
+  bool done = mbar_try_wait(bar, parity);
+  if (!__all_sync(0xFFFFFFFFu, done)) {
+    uint64_t t0 = 0;
+    for (uint32_t it = 1; it < kWaitMaxPolls && !done; ++it) {
+      done = mbar_try_wait(bar, parity);
+      if ((it & 255u) == 0 && !done) {
+        if (*abort_flag) break;
+        const uint64_t t = global_timer_ns();
+        if (t0 == 0) t0 = t;
+        if (t - t0 > kWaitBudgetNs) break;
+      }
+    }
+    if (!done) *abort_flag = 1;
+    done = __all_sync(0xFFFFFFFFu, done);
+  }
+  return done;
+}
+
 // ---------------------------------------------------------------- TMA (no multicast anywhere)
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
@@ -176,6 +197,11 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t local, uint32_t rank) {
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// The same without ordering the thread's memory accesses (a release at cluster scope waits for every load in flight): for handing
+// back tensor memory whose reads tcgen05.wait::ld has completed.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void st_cluster_f32(uint32_t cluster_addr, float a) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(a) : "memory");

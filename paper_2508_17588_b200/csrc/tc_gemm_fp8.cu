@@ -52,27 +52,38 @@ __device__ __forceinline__ float gelu_exact_f(float t) {
 template <int OUT>
 __device__ __forceinline__ float gelu(float t) { return OUT == kOutBf16 ? gelu_tanh_f(t) : gelu_exact_f(t); }
 
-// Wait for 16 columns asked for with tmem_ld16; the registers are named so that nothing that uses them moves ahead of it.
-__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+// Wait for columns asked for with tmem_ld; the registers are named so that nothing that uses them moves ahead of it.
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
                :
                : "memory");
 }
-// acc += s * (NC columns of this thread's TMEM lane), 16 columns on their way while 16 are added.
-template <int NC>
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+// acc += s * (NC columns of this thread's TMEM lane), CH columns on their way while CH are added.
+template <int NC, int CH>
 __device__ __forceinline__ void promote(float2 (&acc)[NC / 2], uint32_t taddr, float s) {
-  uint32_t r[2][16];
+  uint32_t r[2][CH];
   const float2 s2 = make_float2(s, s);
-  tmem_ld16(taddr, r[0]);
+  tmem_ld(taddr, r[0]);
 #pragma unroll
-  for (int c = 0; c < NC / 16; ++c) {
-    tmem_wait16(r[c & 1]);
-    if (c + 1 < NC / 16) tmem_ld16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
+  for (int c = 0; c < NC / CH; ++c) {
+    tmem_wait(r[c & 1]);
+    if (c + 1 < NC / CH) tmem_ld(taddr + (c + 1) * CH, r[(c + 1) & 1]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      acc[c * 8 + i] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), s2, acc[c * 8 + i]);
+    for (int i = 0; i < CH / 2; ++i) {
+      float2& a = acc[c * (CH / 2) + i];
+      a = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), s2, a);
+    }
   }
 }
 // The same with a factor per column: that of column c is lane c's `s` (columns 32 and on: lane c - 32's `s_hi`).
@@ -89,13 +100,46 @@ __device__ __forceinline__ void promote_columns(float2 (&acc)[NC / 2], uint32_t 
       const float from = col < 32 ? s : s_hi;
       f[i] = make_float2(__shfl_sync(0xFFFFFFFFu, from, col & 31), __shfl_sync(0xFFFFFFFFu, from, (col + 1) & 31));
     }
-    tmem_wait16(r[c & 1]);
+    tmem_wait(r[c & 1]);
     if (c + 1 < NC / 16) tmem_ld16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       acc[c * 8 + i] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), f[i], acc[c * 8 + i]);
   }
 }
+
+// The scales of A that a warp needs, R rows by the next 16 K blocks, in shared memory of its own.  A row's scales lie side by side
+// and the rows do not: 16 lanes fetch 16 blocks of one row (64 bytes) and put them down transposed, so that lane r then finds its
+// row's scales block by block without bank conflicts.  A thread that loads its own row's scale, block by block, touches 32 lines a
+// load: 8774 x 12288 x 3072 took 672 us when it asked one block ahead, and the loads alone kept the promotion from its pace
+// when it asked seven ahead.  Two windows: one is filled while the other is used.
+constexpr int kWindow = 16;
+template <int R>
+struct ScaleWindow {
+  static constexpr int kFloats = 2 * kWindow * (R + 1);
+  float* buf;
+  const float* scale;            // of A
+  int M, k_blocks, lane;
+  // Rows row0.. (past the end: the last one's), blocks kb0..kb0 + 15 as far as they go below kb_end, into window w.
+  __device__ __forceinline__ void fetch(uint32_t w, int row0, int kb0, int kb_end) const {
+    const int c = lane & (kWindow - 1), kb = kb0 + c;
+    if (kb < kb_end) {
+      const uint32_t to = smem_u32(buf + ((w & 1) * kWindow + c) * (R + 1));
+#pragma unroll
+      for (int i = 0; i < R / 2; ++i) {
+        const int r = 2 * i + (lane >> 4);
+        const float* from = scale + (long long)min(row0 + r, M - 1) * k_blocks + kb;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + r * 4), "l"(from) : "memory");
+      }
+    }
+  }
+  // All that was asked for is there, for every lane of the warp.
+  static __device__ __forceinline__ void arrived() {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+  }
+  __device__ __forceinline__ float at(uint32_t w, int c, int r) const { return buf[((w & 1) * kWindow + c) * (R + 1) + r]; }
+};
 
 // A warp puts NC bias values from column n0 on into its own piece of shared memory, in fp32; zeros past the end of the row and
 // where there is no bias.
@@ -224,16 +268,18 @@ struct SplitCfg {
   static constexpr int kThreads = 64 + 32 * kWarps;
   static constexpr int kCols = SWAP ? BN : BN / 2;             // of a warp
   static constexpr int kStageBytes = kRowBytes + BN * kStepK;
-  static constexpr int kStages = !SWAP ? (BN == 128 ? 4 : 6) : (BN == 16 ? 5 : (BN == 32 ? 4 : 3));
+  static constexpr int kStages = !SWAP ? (BN == 128 ? 4 : 5) : (BN == 16 ? 5 : (BN == 32 ? 4 : 3));
   static constexpr int kTmemCols = 2 * BN;                     // (a power of two, at least 32)
   static constexpr int kMaxSplit = SWAP ? 8 : 4;
   static constexpr size_t kBiasBytes = SWAP ? 0 : (size_t)kWarps * kCols * 4;
   static constexpr size_t kAmaxBytes = SWAP ? (size_t)4 * BN * 4 : (size_t)2 * kRows * 4;
+  static constexpr int kScaleRows = SWAP ? BN : 32;            // rows of A whose scales a warp needs
+  static constexpr size_t kScaleBytes = (size_t)kWarps * ScaleWindow<kScaleRows>::kFloats * 4;
   static constexpr size_t part_bytes(int split) {              // columns of A's rows, or 128 / split rows, from each of the others
     return SWAP ? (size_t)(split - 1) * (BN / split) * kRows * 4 : (size_t)(split - 1) * (kRows / split) * BN * 4;
   }
   static constexpr size_t smem(int split) {
-    return kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kAmaxBytes + kBarrierBytes + part_bytes(split);
+    return kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kAmaxBytes + kScaleBytes + kBarrierBytes + part_bytes(split);
   }
 };
 
@@ -247,7 +293,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
   uint32_t* s_amax = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_amax) + Cfg::kAmaxBytes);
+  float* s_scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_amax) + Cfg::kAmaxBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
   uint64_t* full = bars;                    // [kStages] TMA -> MMA
   uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA
   uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion
@@ -332,31 +379,37 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     if constexpr (!SWAP) stage_bias<kCols>(s_bias, g.bias, n0 + half * kCols, g.N, lane);
 #pragma unroll
     for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
-    // Scales are fetched a block ahead.  Rows and blocks past the end take the last one's (what they scale is not stored).
+    using Window = ScaleWindow<Cfg::kScaleRows>;
+    const Window window = {s_scale + (size_t)(warp - 2) * Window::kFloats, g.a_scale, g.M, k_blocks, lane};
     const float* sw = g.w_scale + (long long)(n0 / kF8Block) * k_blocks;
-    const int row = SWAP ? min(m0 + lane, g.M - 1) : min(m0 + tile_row, g.M - 1);
-    const float* sa = g.a_scale + (long long)row * k_blocks;
-    const float* sa_hi = g.a_scale + (long long)min(m0 + 32 + lane, g.M - 1) * k_blocks;      // SWAP, rows 32 and on
-    float f = 0.f, f_hi = 0.f;
-    if (kb0 < kb1) {
-      f = __ldg(sa + kb0) * __ldg(sw + kb0);
-      if (SWAP && BN > 32) f_hi = __ldg(sa_hi + kb0) * __ldg(sw + kb0);
-    }
+    const int row0 = SWAP ? m0 : m0 + quad * 32, mine = SWAP && BN < 32 ? lane & (BN - 1) : lane;
+    float w16 = 0.f, w16_next = 0.f;           // W's scales of a window, lane c that of block c
+    auto fetch = [&](uint32_t w, int kb) {
+      window.fetch(w, row0, kb, kb1);
+      if (lane < kWindow && kb + lane < kb1) w16_next = __ldg(sw + kb + lane);
+    };
+    fetch(0, kb0);
     for (int kb = kb0; kb < kb1; ++kb) {
-      const int j = kb - kb0, buf = j & 1, ahead = min(kb + 1, kb1 - 1);
-      const float w_next = __ldg(sw + ahead), a_next = __ldg(sa + ahead);
-      float hi_next = 0.f;
-      if (SWAP && BN > 32) hi_next = __ldg(sa_hi + ahead);
+      const int j = kb - kb0, buf = j & 1, c = j & (kWindow - 1);
+      const uint32_t w = (uint32_t)j / kWindow;
+      if (c == 0) {
+        Window::arrived();
+        w16 = w16_next;
+        fetch(w + 1, kb + kWindow);
+      }
+      const float w_scale = __shfl_sync(0xFFFFFFFFu, w16, c);
+      const float f = window.at(w, c, mine) * w_scale;
+      float f_hi = 0.f;
+      if constexpr (SWAP && BN > 32) f_hi = window.at(w, c, 32 + lane) * w_scale;
       if (!(ok = mbar_wait_warp(&acc_full[buf], (j >> 1) & 1, abort_flag))) break;
       tc_fence_after();
       if constexpr (SWAP) promote_columns<kCols>(acc, t_row + buf * BN, f, f_hi);
-      else promote<kCols>(acc, t_row + buf * BN, f);
+      else promote<kCols, 16>(acc, t_row + buf * BN, f);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[buf]);
-      f = a_next * w_next;
-      f_hi = hi_next * w_next;
     }
+    Window::arrived();
   }
 
   // ---------------------------------------------------------------- partial sums
@@ -461,41 +514,49 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Persistent clusters of two CTAs, one per pair of SMs, on tiles of 256 x BN: each CTA fetches its own 128 rows of A and half
-// of the tile's rows of W, a K step of 128 costs an SM 32 KB from L2 (BN = 256) for the 8.4 MFLOP it computes.
-//   warp 0      TMA producer (both CTAs, each its own operand rows; all bytes reported to the even CTA's barrier)
-//   warp 1      MMA issuer (even CTA only): 4 x tcgen05.mma M256 N=BN K32 per block into one of two TMEM buffers; the commits
-//               free both CTAs' stage and hand the buffer to both CTAs' promotion
-//   warps 2..9  promotion and epilogue (both CTAs, each its own 128 rows; two warps share 32 rows, half of the columns each)
+// Persistent clusters of two CTAs, one per pair of SMs, on tiles of 256 x 256: each CTA fetches its own 128 rows of A and half
+// of the tile's rows of W, a K step of 128 costs an SM 32 KB from L2 for the 8.4 MFLOP it computes.
+//   warp 0       TMA producer (both CTAs, each its own operand rows; all bytes reported to the even CTA's barrier)
+//   warps 1, 2   MMA issuers (even CTA only), one for each half of the tile's columns: 4 x tcgen05.mma M256 N128 K32 per block
+//                into one of the half's two TMEM buffers; the commits free both CTAs' stage and hand the buffer to both CTAs
+//   warp 3       tensor memory
+//   warps 4..11  promotion and epilogue (both CTAs, each its own 128 rows): a warpgroup for each half of the columns
+// A buffer's round trip (MMAs, commit, promotion, hand-back through the other CTA's shared memory) is longer than a block's MMAs;
+// the halves have barriers of their own so that one half's MMAs run while the other half's buffers travel.
 // ---------------------------------------------------------------------------------------------------------------
-template <int BN>
 struct PairCfg {
-  static constexpr int kWarps = 8, kThreads = 320, kCols = BN / 2;
-  static constexpr int kStageBytes = kRowBytes + BN / 2 * kStepK;
-  static constexpr int kStages = 196608 / kStageBytes;         // 192 KB: 6 (BN = 256) or 8 (BN = 128)
-  static constexpr int kTmemCols = 2 * BN;
+  static constexpr int kBN = 256, kCols = 128;                 // of a tile, of a warp
+  static constexpr int kWarps = 8, kThreads = 384;
+  static constexpr int kStageBytes = kRowBytes + kBN / 2 * kStepK;
+  static constexpr int kStages = 5;                            // 160 KB
+  static constexpr int kTmemCols = 512;
   static constexpr size_t kBiasBytes = (size_t)kWarps * kCols * 4;
-  static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kBarrierBytes;
+  static constexpr size_t kScaleBytes = (size_t)kWarps * ScaleWindow<32>::kFloats * 4;
+  static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kScaleBytes + kBarrierBytes;
+  // Registers: 384 threads start with 168 each; the first warpgroup gives up what the other two, with 128 sums a thread, take
+  // (128 * 56 + 256 * 224 = 384 * 168).
+  static constexpr int kFewRegs = 56, kManyRegs = 224;
+  static constexpr int kPromote = 16;                          // columns a TMEM read
 };
 
-template <int BN, int OUT>
-__global__ void __launch_bounds__(PairCfg<BN>::kThreads, 1)
+template <int OUT>
+__global__ void __launch_bounds__(PairCfg::kThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const F8Gemm g,
                 int* __restrict__ status) {
-  static_assert(OUT != kOutF8 || BN == 256, "a thread holds a whole block of an e4m3 result");
-  using Cfg = PairCfg<BN>;
-  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols;
+  using Cfg = PairCfg;
+  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols, BN = Cfg::kBN, kPromote = Cfg::kPromote;
   extern __shared__ uint8_t smem_raw[];
   // The dynamic shared memory starts at the same offset in both CTAs, and so does everything carved from it: a
   // descriptor or a barrier offset means the same place in either.
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
+  float* s_scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
   uint64_t* full = bars;                    // [kStages] both CTAs' TMA -> MMA (the even CTA's is the one in use)
-  uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA (each CTA its own)
-  uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion (each CTA its own)
-  uint64_t* acc_empty = acc_full + 2;       // [2] both CTAs' promotion -> MMA (the even CTA's)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* empty = bars + kStages;         // [kStages] both issuers -> TMA (each CTA its own)
+  uint64_t* acc_full = bars + 2 * kStages;  // [half][2] MMA -> promotion (each CTA its own)
+  uint64_t* acc_empty = acc_full + 4;       // [half][2] both CTAs' promotion -> MMA (the even CTA's)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -506,13 +567,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   const int k_blocks = (g.K - 1) / kStepK + 1;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * Cfg::kWarps); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
+    for (int i = 0; i < 4; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kWarps); }
     *abort_flag = 0;
     mbar_fence_init();
   }
   if (warp == 0 && lane == 0) { tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_w); }
-  if (warp == 1) tmem_alloc_pair(tmem_slot, Cfg::kTmemCols);
+  if (warp == 3) tmem_alloc_pair(tmem_slot, Cfg::kTmemCols);
   tc_fence_before();
   __syncwarp();
   cluster_sync();                           // both CTAs' barriers exist before anybody signals across
@@ -520,15 +581,17 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   const uint32_t tmem_base = *tmem_slot;
   stream_order();
 
-  if (warp == 0) {
-    // ------------------------------------------------------------ TMA producer
-    if (lane == 0) {
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Cfg::kFewRegs));
+    if (warp == 0 && lane == 0) {
+      // ------------------------------------------------------------ TMA producer
       int stage = 0; uint32_t phase = 0;
       bool ok = true;
       for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
         int mt, nt;
         tile_coords(tile, m_tiles, n_tiles, mt, nt);
-        const int row_a = (2 * mt + (int)rank) * kRows, row_w = nt * BN + (int)rank * (BN / 2);
+        // Of the 128 columns of a half the even CTA has the rows of W for the first 64, the odd one for the others.
+        const int row_a = (2 * mt + (int)rank) * kRows, row_w = nt * BN + (int)rank * (kCols / 2);
         for (int kb = 0; kb < k_blocks; ++kb) {
           if (!(ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag))) break;
           // The even CTA's barrier counts the bytes of both CTAs.  The odd CTA's may land before it is armed: its
@@ -537,6 +600,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
           const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes), bar = cluster_map(smem_u32(&full[stage]), 0);
           tma_load_2d_pair(sa, &tm_a, bar, kb * kStepK, row_a);
           tma_load_2d_pair(sa + kRowBytes, &tm_w, bar, kb * kStepK, row_w);
+          tma_load_2d_pair(sa + kRowBytes + kRowBytes / 2, &tm_w, bar, kb * kStepK, row_w + kCols);
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -546,68 +610,103 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
         if (++stage == kStages) { stage = 0; phase ^= 1; }
       }
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer (even CTA)
-    if (rank == 0) {
+    } else if ((warp == 1 || warp == 2) && rank == 0) {
+      // ------------------------------------------------------------ MMA issuers (even CTA)
       const bool leader = elect_one();
-      constexpr uint32_t idesc = idesc_e4m3(2 * kRows, BN);
+      const int half = warp - 1;
+      constexpr uint32_t idesc = idesc_e4m3(2 * kRows, BN / 2);
       int stage = 0; uint32_t phase = 0;
       bool ok = true;
       uint32_t j = 0;                        // K blocks so far
       for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
         for (int kb = 0; kb < k_blocks; ++kb, ++j) {
           const uint32_t buf = j & 1;
-          if (!(ok = mbar_wait_warp(&acc_empty[buf], ((j >> 1) & 1) ^ 1, abort_flag))) break;
-          if (!(ok = mbar_wait_warp(&full[stage], phase, abort_flag))) break;
+          if (!(ok = mbar_wait_warp_inline(&full[stage], phase, abort_flag))) break;
+          if (!(ok = mbar_wait_warp_inline(&acc_empty[2 * half + buf], ((j >> 1) & 1) ^ 1, abort_flag))) break;
           tc_fence_after();
           const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes);
-          const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes, 1024);
+          const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes + half * (kRowBytes / 2), 1024);
           if (leader) {
 #pragma unroll
             for (int k = 0; k < kStepK / 32; ++k)
-              mma_f8_ss_pair(tmem_base + buf * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
+              mma_f8_ss_pair(tmem_base + (2 * half + buf) * kCols, da + 2 * k, db + 2 * k, idesc, k != 0);
             mma_commit_pair(&empty[stage]);
-            mma_commit_pair(&acc_full[buf]);
+            mma_commit_pair(&acc_full[2 * half + buf]);
           }
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
     }
   } else {
-    // ------------------------------------------------------------ promotion and epilogue (warps 2..9)
+    // ------------------------------------------------------------ promotion and epilogue (warps 4..11)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Cfg::kManyRegs));
     const int quad = warp & 3;                 // TMEM lane quadrant this warp may read
-    const int half = (warp - 2) >> 2;          // which half of the tile's columns it has
-    float* s_bias = s_bias_all + (size_t)(warp - 2) * kCols;
-    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
+    const int half = (warp - 4) >> 2;          // which half of the tile's columns it has
+    float* s_bias = s_bias_all + (size_t)(warp - 4) * kCols;
+    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 2 * kCols);
+    const uint32_t empty_bar = cluster_map(smem_u32(&acc_empty[2 * half]), 0);
+    using Window = ScaleWindow<32>;
+    const Window window = {s_scale + (size_t)(warp - 4) * Window::kFloats, g.a_scale, g.M, k_blocks, lane};
+    float w16 = 0.f, w16_next = 0.f;           // W's scales of a window, lane c that of block c
+    // The windows run ahead of the promotion, across the end of a tile as well.
+    int f_tile = pair, f_kb = 0, f_row = 0;
+    const float* f_w = nullptr;
+    auto fetch = [&](uint32_t w) {
+      if (f_tile >= n_tiles_total) return;
+      if (f_kb == 0) {
+        int mt, nt;
+        tile_coords(f_tile, m_tiles, n_tiles, mt, nt);
+        f_row = (2 * mt + (int)rank) * kRows + quad * 32;
+        f_w = g.w_scale + (long long)(min(nt * BN + half * kCols, g.N - 1) / kF8Block) * k_blocks;
+      }
+      window.fetch(w, f_row, f_kb, k_blocks);
+      if (lane < kWindow && f_kb + lane < k_blocks) w16_next = __ldg(f_w + f_kb + lane);
+      f_kb += kWindow;
+      if (f_kb >= k_blocks) { f_kb = 0; f_tile += n_pairs; }
+    };
+    uint32_t w = 0;                            // windows so far
+    fetch(0);
     bool ok = true;
     uint32_t j = 0;
     for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
       int mt, nt;
       tile_coords(tile, m_tiles, n_tiles, mt, nt);
       const int m = (2 * mt + (int)rank) * kRows + quad * 32 + lane, n_first = nt * BN + half * kCols;
-      stage_bias<kCols>(s_bias, g.bias, n_first, g.N, lane);
-      // Scales are fetched a block ahead.  Rows and blocks past the end take the last one's (what they scale is not stored).
-      const float* sw = g.w_scale + (long long)(min(n_first, g.N - 1) / kF8Block) * k_blocks;
-      const float* sa = g.a_scale + (long long)min(m, g.M - 1) * k_blocks;
-      float f = __ldg(sa) * __ldg(sw);
+      // the bias is asked for now and put into shared memory two blocks later
+      float bias[kCols / 32];
+#pragma unroll
+      for (int i = 0; i < kCols / 32; ++i) {
+        const int n = n_first + i * 32 + lane;
+        bias[i] = g.bias != nullptr && n < g.N ? __bfloat162float(__ldg(g.bias + n)) : 0.f;
+      }
       float2 acc[kCols / 2];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
       for (int kb = 0; kb < k_blocks; ++kb, ++j) {
         const uint32_t buf = j & 1;
-        const int ahead = min(kb + 1, k_blocks - 1);
-        const float a_next = __ldg(sa + ahead), w_next = __ldg(sw + ahead);
-        if (!(ok = mbar_wait_warp(&acc_full[buf], (j >> 1) & 1, abort_flag))) break;
+        const int c = kb & (kWindow - 1);
+        if (c == 0) {
+          Window::arrived();
+          w16 = w16_next;
+          fetch(++w);
+        }
+        const float f = window.at(w - 1, c, lane) * __shfl_sync(0xFFFFFFFFu, w16, c);
+        if (kb == (k_blocks > 2 ? 2 : 0)) {
+          __syncwarp();                        // (all lanes are done with what is there)
+#pragma unroll
+          for (int i = 0; i < kCols / 32; ++i) s_bias[i * 32 + lane] = bias[i];
+          __syncwarp();
+        }
+        if (!(ok = mbar_wait_warp_inline(&acc_full[2 * half + buf], (j >> 1) & 1, abort_flag))) break;
         tc_fence_after();
-        promote<kCols>(acc, t_row + buf * BN, f);
+        promote<kCols, kPromote>(acc, t_row + buf * kCols, f);
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_map(smem_u32(&acc_empty[buf]), 0));
-        f = a_next * w_next;
+        if (lane == 0) mbar_arrive_cluster_relaxed(empty_bar + buf * 8);
       }
       if (ok) emit_row<kCols, OUT>(acc, g, s_bias, m, n_first, nullptr, 0, half, quad);
     }
+    Window::arrived();
   }
 
   // ---------------------------------------------------------------- teardown
@@ -615,21 +714,20 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   __syncwarp();
   cluster_sync();                            // neither CTA leaves while the other may still reach into it
   if (threadIdx.x == 0 && *abort_flag) atomicExch(status, 1);
-  if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, Cfg::kTmemCols); }
+  if (warp == 3) { tc_fence_after(); tmem_dealloc_pair(tmem_base, Cfg::kTmemCols); }
 }
 
-template <int BN, int OUT>
+template <int OUT>
 int launch_pair(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
   static PerDeviceOnce attr_once;            // the opt-in is a property of the kernel ON a device
   HERO_TRY(per_device_once(attr_once, [](int) {
-    HERO_CUDA_TRY(cudaFuncSetAttribute(fp8_pair_kernel<BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg<BN>::kSmem));
+    HERO_CUDA_TRY(cudaFuncSetAttribute(fp8_pair_kernel<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg::kSmem));
     return HERO_OK;
   }));
-  const long long tiles = (long long)((g.M - 1) / (2 * kRows) + 1) * ((g.N - 1) / BN + 1);
+  const long long tiles = (long long)((g.M - 1) / (2 * kRows) + 1) * ((g.N - 1) / PairCfg::kBN + 1);
   if (tiles > 0x3FFFFFFF) return HERO_ERR_ARG;
   const int pairs = tiles < num_sms() / 2 ? (int)tiles : num_sms() / 2;
-  return launch_kernel(fp8_pair_kernel<BN, OUT>, (unsigned)(2 * pairs), PairCfg<BN>::kThreads, PairCfg<BN>::kSmem, s, 2, tm_a, tm_w, g,
-                       d_status);
+  return launch_kernel(fp8_pair_kernel<OUT>, (unsigned)(2 * pairs), PairCfg::kThreads, PairCfg::kSmem, s, 2, tm_a, tm_w, g, d_status);
 }
 
 template <int BN, bool SWAP, int OUT>
@@ -650,11 +748,7 @@ int launch_split(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm&
 
 template <int OUT>
 int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
-  if (plan.split == 0) {
-    if constexpr (OUT != kOutF8)
-      if (plan.bn == 128) return launch_pair<128, OUT>(tm_a, tm_w, g, d_status, s);
-    return launch_pair<256, OUT>(tm_a, tm_w, g, d_status, s);
-  }
+  if (plan.split == 0) return launch_pair<OUT>(tm_a, tm_w, g, d_status, s);
   if (plan.swap) {
     switch (plan.bn) {
       case 16: return launch_split<16, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
@@ -691,7 +785,7 @@ int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const
   const TcGemmF8Plan plan = plan_tc_gemm_fp8(M, Nout, K, out_dtype == HERO_DTYPE_E4M3, num_sms());
   CUtensorMap tm_a, tm_w;
   HERO_TRY(make_tmap_bytes(&tm_a, a, (uint64_t)M, (uint64_t)K, plan.swap ? plan.bn : kRows));
-  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? plan.bn / 2 : (plan.swap ? kRows : plan.bn)));
+  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? PairCfg::kCols / 2 : (plan.swap ? kRows : plan.bn)));
   F8Gemm g = {a_scale, w_scale, static_cast<const __nv_bfloat16*>(bias), c, c_scale, M, Nout, K, act, 0};
   const unsigned long long low = (unsigned long long)reinterpret_cast<uintptr_t>(c) |
                                  (unsigned long long)Nout * (out_dtype == HERO_DTYPE_FP32 ? 4 : (out_dtype == HERO_DTYPE_BF16 ? 2 : 1));
