@@ -113,21 +113,21 @@ __device__ __forceinline__ void promote_columns(float2 (&acc)[NC / 2], uint32_t 
 // row's scales block by block without bank conflicts.  A thread that loads its own row's scale, block by block, touches 32 lines a
 // load: 8774 x 12288 x 3072 took 672 us when it asked one block ahead, and the loads alone kept the promotion from its pace
 // when it asked seven ahead.  Two windows: one is filled while the other is used.
-constexpr int kWindow = 16;
-template <int R>
+template <int R, int W>
 struct ScaleWindow {
-  static constexpr int kFloats = 2 * kWindow * (R + 1);
+  static constexpr int kBlocks = W;
+  static constexpr int kFloats = 2 * W * (R + 1);
   float* buf;
   const float* scale;            // of A
   int M, k_blocks, lane;
-  // Rows row0.. (past the end: the last one's), blocks kb0..kb0 + 15 as far as they go below kb_end, into window w.
+  // Rows row0.. (past the end: the last one's), blocks from kb0 on as far as they go below kb_end, into window w.
   __device__ __forceinline__ void fetch(uint32_t w, int row0, int kb0, int kb_end) const {
-    const int c = lane & (kWindow - 1), kb = kb0 + c;
+    const int c = lane & (W - 1), kb = kb0 + c;
     if (kb < kb_end) {
-      const uint32_t to = smem_u32(buf + ((w & 1) * kWindow + c) * (R + 1));
+      const uint32_t to = smem_u32(buf + ((w & 1) * W + c) * (R + 1));
 #pragma unroll
-      for (int i = 0; i < R / 2; ++i) {
-        const int r = 2 * i + (lane >> 4);
+      for (int i = 0; i < R * W / 32; ++i) {
+        const int r = i * (32 / W) + lane / W;
         const float* from = scale + (long long)min(row0 + r, M - 1) * k_blocks + kb;
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + r * 4), "l"(from) : "memory");
       }
@@ -138,7 +138,28 @@ struct ScaleWindow {
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
   }
-  __device__ __forceinline__ float at(uint32_t w, int c, int r) const { return buf[((w & 1) * kWindow + c) * (R + 1) + r]; }
+  __device__ __forceinline__ float at(uint32_t w, int c, int r) const { return buf[((w & 1) * W + c) * (R + 1) + r]; }
+};
+
+// The same for a whole tile of 128 rows of A by 256 rows of W, filled by a warp that does nothing else: scale of row r at block c,
+// and of the two blocks of W.
+struct ScaleBlock {
+  static constexpr int kBlocks = 16, kLd = kRows + 1;          // (a column more: the writer's lanes go to different banks)
+  static constexpr int kFloats = kBlocks * kLd + 2 * kBlocks;
+  static __device__ __forceinline__ int a_at(int c, int r) { return c * kLd + r; }
+  static __device__ __forceinline__ int w_at(int c, int half) { return kBlocks * kLd + half * kBlocks + c; }
+  // Rows and blocks past the end take the last one's scales (what they scale is not stored).
+  static __device__ __forceinline__ void fetch(float* to, const F8Gemm& g, int row0, int n0, int kb0, int k_blocks, int lane) {
+    const int c = lane & (kBlocks - 1), kb = kb0 + c;
+    if (kb >= k_blocks) return;
+    const uint32_t a = smem_u32(to + a_at(c, 0)), w = smem_u32(to + w_at(c, lane / kBlocks));
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(w),
+                 "l"(g.w_scale + (long long)(min(n0 + lane / kBlocks * kF8Block, g.N - 1) / kF8Block) * k_blocks + kb) : "memory");
+#pragma unroll 8
+    for (int r = lane / kBlocks; r < kRows; r += 32 / kBlocks)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(a + r * 4),
+                   "l"(g.a_scale + (long long)min(row0 + r, g.M - 1) * k_blocks + kb) : "memory");
+  }
 };
 
 // A warp puts NC bias values from column n0 on into its own piece of shared memory, in fp32; zeros past the end of the row and
@@ -231,27 +252,41 @@ __device__ __forceinline__ void store_row(const float2 (&acc)[NC / 2], const F8G
     }
   }
 }
-// Finish and store NC columns of a row.  e4m3: the two warps of a TMEM quadrant that hold halves of a block trade their maxima
-// through `s_amax` (two words a row); NC = 128 is a block by itself.
+// Finish and store NC columns of a row.  e4m3: the two warps that hold the halves of a block trade their maxima through `s_amax`
+// (two words a row) and `meet`, a barrier of theirs for two arrivals, `turn` the parity of its phase; the wait is bounded like every
+// other.
 template <int NC, int OUT>
-__device__ __forceinline__ void emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, uint32_t* s_amax,
-                                         int tile_row, int half, int quad) {
+__device__ __forceinline__ void emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0) {
+  static_assert(NC == kF8Block, "a thread holds a whole block of an e4m3 result");
   finish_row<NC, OUT>(acc, s_bias, g.act);
   float inv = 0.f;
   if constexpr (OUT == kOutF8) {
-    uint32_t amax = row_amax<NC>(acc);
-    if constexpr (NC < kF8Block) {
-      static_assert(2 * NC == kF8Block, "two warps hold a block");
-      s_amax[2 * tile_row + half] = amax;
-      asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
-      amax = max(amax, s_amax[2 * tile_row + (half ^ 1)]);
-      asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");      // (the words are free for the next tile)
-    }
-    const F8Scale s = f8_scale(amax);
+    const F8Scale s = f8_scale(row_amax<NC>(acc));
     inv = s.inv;
-    if (m < g.M && n0 < g.N && n0 % kF8Block == 0) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
+    if (m < g.M && n0 < g.N) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
   }
   if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
+}
+template <int NC, int OUT>
+__device__ __forceinline__ bool emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, uint32_t* s_amax,
+                                         uint64_t* meet, uint32_t turn, int which, volatile int* abort_flag) {
+  finish_row<NC, OUT>(acc, s_bias, g.act);
+  float inv = 0.f;
+  if constexpr (OUT == kOutF8) {
+    static_assert(2 * NC == kF8Block, "two warps hold a block");
+    uint32_t amax = row_amax<NC>(acc);
+    const int lane = threadIdx.x & 31;
+    s_amax[which * 32 + lane] = amax;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(meet);
+    if (!mbar_wait_warp_inline(meet, turn, abort_flag)) return false;
+    amax = max(amax, s_amax[(which ^ 1) * 32 + lane]);
+    const F8Scale s = f8_scale(amax);
+    inv = s.inv;
+    if (m < g.M && n0 < g.N && which == 0) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
+  }
+  if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
+  return true;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -274,7 +309,7 @@ struct SplitCfg {
   static constexpr size_t kBiasBytes = SWAP ? 0 : (size_t)kWarps * kCols * 4;
   static constexpr size_t kAmaxBytes = SWAP ? (size_t)4 * BN * 4 : (size_t)2 * kRows * 4;
   static constexpr int kScaleRows = SWAP ? BN : 32;            // rows of A whose scales a warp needs
-  static constexpr size_t kScaleBytes = (size_t)kWarps * ScaleWindow<kScaleRows>::kFloats * 4;
+  static constexpr size_t kScaleBytes = (size_t)kWarps * ScaleWindow<kScaleRows, 16>::kFloats * 4;
   static constexpr size_t part_bytes(int split) {              // columns of A's rows, or 128 / split rows, from each of the others
     return SWAP ? (size_t)(split - 1) * (BN / split) * kRows * 4 : (size_t)(split - 1) * (kRows / split) * BN * 4;
   }
@@ -299,7 +334,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA
   uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion
   uint64_t* acc_empty = acc_full + 2;       // [2] promotion -> MMA
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* meet = acc_empty + 2;           // [4] the two warps of a quadrant (e4m3 results)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(meet + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* s_part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kBarrierBytes);
 
@@ -315,6 +351,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kWarps); }
+    for (int i = 0; i < 4; ++i) mbar_init(&meet[i], 2);
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -379,7 +416,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     if constexpr (!SWAP) stage_bias<kCols>(s_bias, g.bias, n0 + half * kCols, g.N, lane);
 #pragma unroll
     for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
-    using Window = ScaleWindow<Cfg::kScaleRows>;
+    using Window = ScaleWindow<Cfg::kScaleRows, 16>;
+    constexpr int kWindow = Window::kBlocks;
     const Window window = {s_scale + (size_t)(warp - 2) * Window::kFloats, g.a_scale, g.M, k_blocks, lane};
     const float* sw = g.w_scale + (long long)(n0 / kF8Block) * k_blocks;
     const int row0 = SWAP ? m0 : m0 + quad * 32, mine = SWAP && BN < 32 ? lane & (BN - 1) : lane;
@@ -466,10 +504,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   // ---------------------------------------------------------------- epilogue
   if (warp >= 2) {
     if constexpr (!SWAP) {
-      // (e4m3: the two warps of a quadrant meet in emit_row, so they enter it whatever became of their waits; a row that does
-      // not exist is not stored)
-      if (owner == rank)
-        emit_row<kCols, OUT>(acc, g, s_bias, ok ? m0 + tile_row : g.M, n0 + half * kCols, s_amax, tile_row, half, quad);
+      if (owner == rank && ok)
+        ok = emit_row<kCols, OUT>(acc, g, s_bias, m0 + tile_row, n0 + half * kCols, s_amax + quad * 64, meet + quad, 0, half, abort_flag);
     } else {
       const int n = n0 + tile_row;
       const float b = g.bias != nullptr && n < g.N ? __bfloat162float(__ldg(g.bias + n)) : 0.f;
@@ -519,7 +555,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 //   warp 0       TMA producer (both CTAs, each its own operand rows; all bytes reported to the even CTA's barrier)
 //   warps 1, 2   MMA issuers (even CTA only), one for each half of the tile's columns: 4 x tcgen05.mma M256 N128 K32 per block
 //                into one of the half's two TMEM buffers; the commits free both CTAs' stage and hand the buffer to both CTAs
-//   warp 3       tensor memory
+//   warp 3       tensor memory; then the scales, 16 K blocks at a time
 //   warps 4..11  promotion and epilogue (both CTAs, each its own 128 rows): a warpgroup for each half of the columns
 // A buffer's round trip (MMAs, commit, promotion, hand-back through the other CTA's shared memory) is longer than a block's MMAs;
 // the halves have barriers of their own so that one half's MMAs run while the other half's buffers travel.
@@ -528,15 +564,15 @@ struct PairCfg {
   static constexpr int kBN = 256, kCols = 128;                 // of a tile, of a warp
   static constexpr int kWarps = 8, kThreads = 384;
   static constexpr int kStageBytes = kRowBytes + kBN / 2 * kStepK;
-  static constexpr int kStages = 5;                            // 160 KB
+  static constexpr int kStages = 6;                            // 192 KB
   static constexpr int kTmemCols = 512;
   static constexpr size_t kBiasBytes = (size_t)kWarps * kCols * 4;
-  static constexpr size_t kScaleBytes = (size_t)kWarps * ScaleWindow<32>::kFloats * 4;
+  static constexpr size_t kScaleBytes = 2 * ScaleBlock::kFloats * 4;
   static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kScaleBytes + kBarrierBytes;
   // Registers: 384 threads start with 168 each; the first warpgroup gives up what the other two, with 128 sums a thread, take
-  // (128 * 56 + 256 * 224 = 384 * 168).
-  static constexpr int kFewRegs = 56, kManyRegs = 224;
-  static constexpr int kPromote = 16;                          // columns a TMEM read
+  // (128 * 40 + 256 * 232 = 384 * 168).
+  static constexpr int kFewRegs = 40, kManyRegs = 232;
+  static constexpr int kPromote = 32;                          // columns a TMEM read
 };
 
 template <int OUT>
@@ -544,7 +580,7 @@ __global__ void __launch_bounds__(PairCfg::kThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const F8Gemm g,
                 int* __restrict__ status) {
   using Cfg = PairCfg;
-  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols, BN = Cfg::kBN, kPromote = Cfg::kPromote;
+  constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols, BN = Cfg::kBN, kPromote = Cfg::kPromote, kWindow = ScaleBlock::kBlocks;
   extern __shared__ uint8_t smem_raw[];
   // The dynamic shared memory starts at the same offset in both CTAs, and so does everything carved from it: a
   // descriptor or a barrier offset means the same place in either.
@@ -556,7 +592,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   uint64_t* empty = bars + kStages;         // [kStages] both issuers -> TMA (each CTA its own)
   uint64_t* acc_full = bars + 2 * kStages;  // [half][2] MMA -> promotion (each CTA its own)
   uint64_t* acc_empty = acc_full + 4;       // [half][2] both CTAs' promotion -> MMA (the even CTA's)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 4);
+  uint64_t* sc_full = acc_empty + 4;        // [2] scales -> promotion
+  uint64_t* sc_empty = sc_full + 2;         // [2] promotion -> scales
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -569,6 +607,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
     for (int i = 0; i < 4; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kWarps); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sc_full[i], 32); mbar_init(&sc_empty[i], Cfg::kWarps); }
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -636,6 +675,20 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
+    } else if (warp == 3) {
+      // ------------------------------------------------------------ scales
+      uint32_t w = 0;                        // windows so far
+      bool ok = true;
+      for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
+        int mt, nt;
+        tile_coords(tile, m_tiles, n_tiles, mt, nt);
+        for (int kb = 0; kb < k_blocks; kb += kWindow, ++w) {
+          if (!(ok = mbar_wait_warp(&sc_empty[w & 1], ((w >> 1) & 1) ^ 1, abort_flag))) break;
+          ScaleBlock::fetch(s_scale + (w & 1) * ScaleBlock::kFloats, g, (2 * mt + (int)rank) * kRows, nt * BN, kb, k_blocks, lane);
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sc_full[w & 1])) : "memory");
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
   } else {
     // ------------------------------------------------------------ promotion and epilogue (warps 4..11)
@@ -645,27 +698,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     float* s_bias = s_bias_all + (size_t)(warp - 4) * kCols;
     const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 2 * kCols);
     const uint32_t empty_bar = cluster_map(smem_u32(&acc_empty[2 * half]), 0);
-    using Window = ScaleWindow<32>;
-    const Window window = {s_scale + (size_t)(warp - 4) * Window::kFloats, g.a_scale, g.M, k_blocks, lane};
-    float w16 = 0.f, w16_next = 0.f;           // W's scales of a window, lane c that of block c
-    // The windows run ahead of the promotion, across the end of a tile as well.
-    int f_tile = pair, f_kb = 0, f_row = 0;
-    const float* f_w = nullptr;
-    auto fetch = [&](uint32_t w) {
-      if (f_tile >= n_tiles_total) return;
-      if (f_kb == 0) {
-        int mt, nt;
-        tile_coords(f_tile, m_tiles, n_tiles, mt, nt);
-        f_row = (2 * mt + (int)rank) * kRows + quad * 32;
-        f_w = g.w_scale + (long long)(min(nt * BN + half * kCols, g.N - 1) / kF8Block) * k_blocks;
-      }
-      window.fetch(w, f_row, f_kb, k_blocks);
-      if (lane < kWindow && f_kb + lane < k_blocks) w16_next = __ldg(f_w + f_kb + lane);
-      f_kb += kWindow;
-      if (f_kb >= k_blocks) { f_kb = 0; f_tile += n_pairs; }
-    };
-    uint32_t w = 0;                            // windows so far
-    fetch(0);
+    uint32_t w = 0;                            // windows of scales so far
     bool ok = true;
     uint32_t j = 0;
     for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
@@ -682,31 +715,69 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
       float2 acc[kCols / 2];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
-      for (int kb = 0; kb < k_blocks; ++kb, ++j) {
-        const uint32_t buf = j & 1;
-        const int c = kb & (kWindow - 1);
-        if (c == 0) {
-          Window::arrived();
-          w16 = w16_next;
-          fetch(++w);
+      // The promotion of a block reaches into the next, so that little latency is left between two packed FMAs: the next block's
+      // scales are read while the first columns are added; once the last columns are in registers the buffer goes back and the
+      // first of the next block are asked for.
+      uint32_t r[2][kPromote];
+      const float* scales = s_scale;
+      auto turn = [&]() {                      // into the next window, handing back the last
+        if (w > 0) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_empty[(w - 1) & 1]);
         }
-        const float f = window.at(w - 1, c, lane) * __shfl_sync(0xFFFFFFFFu, w16, c);
-        if (kb == (k_blocks > 2 ? 2 : 0)) {
+        mbar_wait_lane(&sc_full[w & 1], (w >> 1) & 1, abort_flag);
+        scales = s_scale + (w & 1) * ScaleBlock::kFloats;
+        ++w;
+      };
+      turn();
+      float a_next = scales[ScaleBlock::a_at(0, quad * 32 + lane)], w_next = scales[ScaleBlock::w_at(0, half)];
+      mbar_wait_lane(&acc_full[2 * half + (j & 1)], (j >> 1) & 1, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      tmem_ld(t_row + (j & 1) * kCols, r[0]);
+      for (int kb = 0; kb < k_blocks; ++kb) {
+        const uint32_t taddr = t_row + (j & 1) * kCols;
+        const float f = a_next * w_next;
+        const float2 s2 = make_float2(f, f);
+        const bool more = kb + 1 < k_blocks;
+        const int c = (kb + 1) & (kWindow - 1);
+        if (more && c == 0) turn();
+        a_next = scales[ScaleBlock::a_at(c, quad * 32 + lane)];
+        w_next = scales[ScaleBlock::w_at(c, half)];
+        constexpr int kPieces = kCols / kPromote;
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+          tmem_wait(r[q & 1]);
+          if (q + 1 < kPieces) {
+            tmem_ld(taddr + (q + 1) * kPromote, r[(q + 1) & 1]);
+          } else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(empty_bar + (j & 1) * 8);
+            ++j;
+            if (more) {
+              mbar_wait_lane(&acc_full[2 * half + (j & 1)], (j >> 1) & 1, abort_flag);
+              __syncwarp();
+              tc_fence_after();
+              tmem_ld(t_row + (j & 1) * kCols, r[0]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kPromote / 2; ++i) {
+            float2& a = acc[q * (kPromote / 2) + i];
+            a = __ffma2_rn(make_float2(__uint_as_float(r[q & 1][2 * i]), __uint_as_float(r[q & 1][2 * i + 1])), s2, a);
+          }
+        }
+        if (kb == 0) {                         // (the bias has arrived by now)
           __syncwarp();                        // (all lanes are done with what is there)
 #pragma unroll
           for (int i = 0; i < kCols / 32; ++i) s_bias[i * 32 + lane] = bias[i];
           __syncwarp();
         }
-        if (!(ok = mbar_wait_warp_inline(&acc_full[2 * half + buf], (j >> 1) & 1, abort_flag))) break;
-        tc_fence_after();
-        promote<kCols, kPromote>(acc, t_row + buf * kCols, f);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(empty_bar + buf * 8);
       }
-      if (ok) emit_row<kCols, OUT>(acc, g, s_bias, m, n_first, nullptr, 0, half, quad);
+      ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0);
+      if (ok) emit_row<kCols, OUT>(acc, g, s_bias, m, n_first);
     }
-    Window::arrived();
   }
 
   // ---------------------------------------------------------------- teardown
