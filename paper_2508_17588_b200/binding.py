@@ -392,27 +392,31 @@ def _blocks(n: int) -> int:
     return -(-n // 128)
 
 
-def _f8_call(name: str, tensors: dict, args: tuple) -> None:
-    """Check {argument name: (tensor or None, dtype, shape)} and call `name` with `args` and the current stream of the tensors' device.
+def _f8_call(name: str, device: int, tensors: tuple, args: tuple) -> None:
+    """Check (argument name, tensor or None, dtype, shape) of every tensor and call `name` with their addresses, `args` and the current
+    stream of GPU `device`, which need not be the current one.
 
-    Every tensor is contiguous, of the named dtype and shape and on one GPU, which need not be the current one; a HeroError with
-    ERR_ARG says which is not."""
-    device = None
-    for arg, (t, dtype, shape) in tensors.items():
+    Every tensor is contiguous, of its dtype and shape and on that GPU; a HeroError with ERR_ARG says which is not.  (A call of a
+    few microseconds on the GPU is no longer than this function: the checks are the cheapest that torch has.)"""
+    if device < 0:
+        raise HeroError(ERR_ARG, f"{name}: tensors must be on a CUDA device")
+    ptrs = []
+    for arg, t, dtype, shape in tensors:
         if t is None:
+            ptrs.append(0)
             continue
-        if not t.is_cuda:
-            raise HeroError(ERR_ARG, f"{name}: {arg} must be a CUDA tensor")
-        if device is None:
-            device = t.device
-        if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-            raise HeroError(ERR_ARG, f"{name}: {arg} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+        if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise HeroError(ERR_ARG, f"{name}: {arg} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, got "
                                      f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _check(getattr(load(), name)(*args, _stream()), name)
+        ptrs.append(t.data_ptr())
+    call = getattr(load(), name)
+    if device == torch.cuda.current_device():
+        code = call(*ptrs, *args, torch._C._cuda_getCurrentRawStream(device))
     else:
-        _check(getattr(load(), name)(*args, _stream()), name)
+        with torch.cuda.device(device):
+            code = call(*ptrs, *args, torch._C._cuda_getCurrentRawStream(device))
+    if code < 0:
+        raise HeroError(code, name)
 
 
 def _matrix(name: str, arg: str, t, dims: int = 2):
@@ -422,19 +426,22 @@ def _matrix(name: str, arg: str, t, dims: int = 2):
 
 
 def _run_dtype(name: str, t) -> int:
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise HeroError(ERR_ARG, f"{name}: inputs are bf16 or fp32, got {t.dtype}")
-    return DTYPE_BF16 if t.dtype == torch.bfloat16 else DTYPE_FP32
+    if t.dtype is torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype is torch.float32:
+        return DTYPE_FP32
+    raise HeroError(ERR_ARG, f"{name}: inputs are bf16 or fp32, got {t.dtype}")
 
 
 def hero_quantize_fp8(x, q, scale, block_rows: int = 1):
     """q (float8_e4m3fn), scale (fp32) <- x [rows, cols], a scale per row and 128 columns (block_rows=1) or per 128 x 128 elements."""
-    rows, cols = _matrix("hero_quantize_fp8", "x", x)
-    dtype = _run_dtype("hero_quantize_fp8", x)
-    _f8_call("hero_quantize_fp8",
-             {"x": (x, x.dtype, (rows, cols)), "q": (q, F8, (rows, cols)),
-              "scale": (scale, torch.float32, (rows if block_rows == 1 else _blocks(rows), _blocks(cols)))},
-             (_ptr(x), _ptr(q), _ptr(scale), rows, cols, block_rows, dtype))
+    name = "hero_quantize_fp8"
+    rows, cols = shape = _matrix(name, "x", x)
+    dtype = _run_dtype(name, x)
+    _f8_call(name, x.get_device(),
+             (("x", x, x.dtype, shape), ("q", q, F8, shape),
+              ("scale", scale, torch.float32, (rows if block_rows == 1 else _blocks(rows), _blocks(cols)))),
+             (rows, cols, block_rows, dtype))
     return q, scale
 
 
@@ -443,62 +450,73 @@ def hero_gather_ln_modulate_fp8(x, add, idx, shift, scale, out, out_scale):
     shift and scale are fp32 [B, D] with one row stride (they may be slices of one tensor); idx is int32 [n_sel] or None (the
     first n_sel rows), its entries from 0 to N - 1."""
     name = "hero_gather_ln_modulate_fp8"
-    B, N, D = _matrix(name, "x", x, 3)
+    B, N, D = shape = _matrix(name, "x", x, 3)
     n_sel = _matrix(name, "out", out, 3)[1]
-    dtype = _run_dtype(name, x)
+    dtype, device = _run_dtype(name, x), x.get_device()
     for arg, t in (("shift", shift), ("scale", scale)):
-        if t is None or t.dtype != torch.float32 or tuple(t.shape) != (B, D) or t.device != x.device or (D > 1 and t.stride(1) != 1):
+        if t is None or t.dtype is not torch.float32 or t.shape != (B, D) or t.get_device() != device or (D > 1 and t.stride(1) != 1):
             raise HeroError(ERR_ARG, f"{name}: {arg} must be fp32 of shape {(B, D)} on {x.device} with contiguous rows")
     if B > 1 and shift.stride(0) != scale.stride(0):
         raise HeroError(ERR_ARG, f"{name}: shift and scale must have the same row stride")
-    _f8_call(name, {"x": (x, x.dtype, (B, N, D)), "add": (add, x.dtype, (B, N, D)), "idx": (idx, torch.int32, (n_sel,)),
-                    "out": (out, F8, (B, n_sel, D)), "out_scale": (out_scale, torch.float32, (B, n_sel, _blocks(D)))},
-             (_ptr(x), _ptr(add), _ptr(idx), _ptr(shift), _ptr(scale), shift.stride(0) if B > 1 else D, _ptr(out), _ptr(out_scale),
+    # (shift and scale stand between the list and the result in the call: checked above, passed by address)
+    _f8_call(name, device,
+             (("x", x, x.dtype, shape), ("add", add, x.dtype, shape), ("idx", idx, torch.int32, (n_sel,))),
+             (shift.data_ptr(), scale.data_ptr(), shift.stride(0) if B > 1 else D, *_f8_out(name, device, out, out_scale, (B, n_sel, D)),
               B, N, n_sel, D, dtype))
     return out, out_scale
 
 
-def _rms_tensors(name, x, add, gain, sum):
-    rows, D = _matrix(name, "x", x)
-    dtype = _run_dtype(name, x)
-    return rows, D, dtype, {"x": (x, x.dtype, (rows, D)), "add": (add, x.dtype, (rows, D)), "gain": (gain, x.dtype, (D,)),
-                            "sum": (sum, x.dtype, (rows, D))}
+def _f8_out(name, device, out, out_scale, shape):
+    """Addresses of an e4m3 result [.., D] and its scales [.., ceil(D / 128)]."""
+    for arg, t, dtype, want in (("out", out, F8, shape), ("out_scale", out_scale, torch.float32, (*shape[:-1], _blocks(shape[-1])))):
+        if t is None or t.get_device() != device or t.dtype is not dtype or t.shape != want or not t.is_contiguous():
+            raise HeroError(ERR_ARG, f"{name}: {arg} must be a contiguous {dtype} tensor of shape {want} on cuda:{device}")
+    return out.data_ptr(), out_scale.data_ptr()
 
 
 def hero_rms_norm(x, add, gain, sum, out, eps: float = 1e-5):
     """sum <- x + add, out <- (x + add) / sqrt(mean((x + add)^2) + eps) * gain over the rows of [rows, D]; add, gain and sum may be
     None.  sum or out (not both) may be x or add."""
-    rows, D, dtype, tensors = _rms_tensors("hero_rms_norm", x, add, gain, sum)
-    tensors["out"] = (out, x.dtype, (rows, D))
-    _f8_call("hero_rms_norm", tensors, (_ptr(x), _ptr(add), _ptr(gain), _ptr(sum), _ptr(out), rows, D, eps, dtype))
+    name = "hero_rms_norm"
+    rows, D = shape = _matrix(name, "x", x)
+    dt, dtype = x.dtype, _run_dtype(name, x)
+    _f8_call(name, x.get_device(),
+             (("x", x, dt, shape), ("add", add, dt, shape), ("gain", gain, dt, (D,)), ("sum", sum, dt, shape), ("out", out, dt, shape)),
+             (rows, D, eps, dtype))
     return out
 
 
 def hero_rms_norm_fp8(x, add, gain, sum, out, out_scale, eps: float = 1e-5):
     """hero_rms_norm with out in e4m3 (float8_e4m3fn [rows, D]) and a scale per row and 128 columns."""
-    rows, D, dtype, tensors = _rms_tensors("hero_rms_norm_fp8", x, add, gain, sum)
-    tensors["out"] = (out, F8, (rows, D))
-    tensors["out_scale"] = (out_scale, torch.float32, (rows, _blocks(D)))
-    _f8_call("hero_rms_norm_fp8", tensors,
-             (_ptr(x), _ptr(add), _ptr(gain), _ptr(sum), _ptr(out), _ptr(out_scale), rows, D, eps, dtype))
+    name = "hero_rms_norm_fp8"
+    rows, D = shape = _matrix(name, "x", x)
+    dt, dtype = x.dtype, _run_dtype(name, x)
+    _f8_call(name, x.get_device(),
+             (("x", x, dt, shape), ("add", add, dt, shape), ("gain", gain, dt, (D,)), ("sum", sum, dt, shape), ("out", out, F8, shape),
+              ("out_scale", out_scale, torch.float32, (rows, _blocks(D)))),
+             (rows, D, eps, dtype))
     return out, out_scale
+
+
+_GEMM_OUT = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, F8: DTYPE_E4M3}
 
 
 def hero_gemm_fp8(a, a_scale, w, w_scale, bias, c, c_scale=None, act: int = 0):
     """c <- act(A W^T + bias) of e4m3 operands a [M, K] (a_scale [M, ceil(K / 128)]) and w [N, K] (w_scale [ceil(N / 128),
     ceil(K / 128)]); bias bf16 [N] or None, act 1: GELU-tanh.  c is bf16 or fp32 [M, N], or float8_e4m3fn with c_scale [M, ceil(N / 128)]."""
-    M, K = _matrix("hero_gemm_fp8", "a", a)
-    N = _matrix("hero_gemm_fp8", "w", w)[0]
-    _matrix("hero_gemm_fp8", "c", c)
-    out = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, F8: DTYPE_E4M3}.get(c.dtype)
+    name = "hero_gemm_fp8"
+    M, K = _matrix(name, "a", a)
+    N = _matrix(name, "w", w)[0]
+    _matrix(name, "c", c)
+    out = _GEMM_OUT.get(c.dtype)
     if out is None:
-        raise HeroError(ERR_ARG, f"hero_gemm_fp8: c is bf16, fp32 or float8_e4m3fn, got {c.dtype}")
-    kb = _blocks(K)
-    _f8_call("hero_gemm_fp8",
-             {"a": (a, F8, (M, K)), "a_scale": (a_scale, torch.float32, (M, kb)), "w": (w, F8, (N, K)),
-              "w_scale": (w_scale, torch.float32, (_blocks(N), kb)), "bias": (bias, torch.bfloat16, (N,)), "c": (c, c.dtype, (M, N)),
-              "c_scale": (c_scale, torch.float32, (M, _blocks(N)))},
-             (_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(c), _ptr(c_scale), M, N, K, act, out))
+        raise HeroError(ERR_ARG, f"{name}: c is bf16, fp32 or float8_e4m3fn, got {c.dtype}")
+    kb, nb = _blocks(K), _blocks(N)
+    f32 = torch.float32
+    _f8_call(name, a.get_device(),
+             (("a", a, F8, (M, K)), ("a_scale", a_scale, f32, (M, kb)), ("w", w, F8, (N, K)), ("w_scale", w_scale, f32, (nb, kb)),
+              ("bias", bias, torch.bfloat16, (N,)), ("c", c, c.dtype, (M, N)), ("c_scale", c_scale, f32, (M, nb))),
+             (M, N, K, act, out))
     return c
 
 

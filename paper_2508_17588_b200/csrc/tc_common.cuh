@@ -44,20 +44,6 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Whether the phase is over, without waiting for it.
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t"
-      ".reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t"
-      "}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
 // Bounded wait: polls for at most about one second of wall clock (global timer), with a hard
 // cap on iterations as a second line of defence.  `abort_flag` (shared memory) lets one role's
 // failure release every other role promptly.  Returns false on give-up.
@@ -114,11 +100,24 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
 // The same wait without a function call, for code whose registers a call would push out (a warp that holds 128 sums a thread).
 // Each lane by itself: whether it gave up stands in abort_flag alone, for the caller to look at before it stores anything; a wait
 // after that gives up at once.
-__device__ __forceinline__ void mbar_wait_lane(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return;
+__device__ __forceinline__ bool mbar_try_wait_at(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_try_wait_at(bar, parity)) return;
   uint64_t t0 = 0;
   for (uint32_t it = 1; it < kWaitMaxPolls; ++it) {
-    if (mbar_try_wait(bar, parity)) return;
+    if (mbar_try_wait_at(bar, parity)) return;
     if ((it & 63u) == 0) {
       if (*abort_flag) return;
       const uint64_t t = global_timer_ns();
@@ -128,27 +127,6 @@ __device__ __forceinline__ void mbar_wait_lane(uint64_t* bar, uint32_t parity, v
   }
   *abort_flag = 1;
 }
-// The same wait without a function call, for code whose registers a call would push out (a warp that holds 128 sums a thread).
-__device__ __forceinline__ bool mbar_wait_warp_inline(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  __syncwarp();
-  bool done = mbar_try_wait(bar, parity);
-  if (!__all_sync(0xFFFFFFFFu, done)) {
-    uint64_t t0 = 0;
-    for (uint32_t it = 1; it < kWaitMaxPolls && !done; ++it) {
-      done = mbar_try_wait(bar, parity);
-      if ((it & 255u) == 0 && !done) {
-        if (*abort_flag) break;
-        const uint64_t t = global_timer_ns();
-        if (t0 == 0) t0 = t;
-        if (t - t0 > kWaitBudgetNs) break;
-      }
-    }
-    if (!done) *abort_flag = 1;
-    done = __all_sync(0xFFFFFFFFu, done);
-  }
-  return done;
-}
-
 // ---------------------------------------------------------------- TMA (no multicast anywhere)
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");

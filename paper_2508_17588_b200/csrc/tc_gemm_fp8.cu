@@ -11,7 +11,7 @@
 // Two kernels (launch_tc_gemm_fp8 says which runs when):
 //  * fp8_pair_kernel for problems that fill the chip: persistent CTA pairs on 256-row tiles (cta_group::2);
 //  * fp8_split_kernel for the others: one tile per CTA, the K loop cut over the CTAs of a cluster; with few rows of A the roles of
-//    the operands are exchanged, so that a tile is 128 rows of W by 16, 32 or 64 rows of A.
+//    the operands are exchanged, so that a tile is 128 rows of W by 16 rows of A.
 #include <cuda.h>
 
 #include "fp8_common.cuh"
@@ -52,22 +52,13 @@ __device__ __forceinline__ float gelu_exact_f(float t) {
 template <int OUT>
 __device__ __forceinline__ float gelu(float t) { return OUT == kOutBf16 ? gelu_tanh_f(t) : gelu_exact_f(t); }
 
-// Wait for columns asked for with tmem_ld; the registers are named so that nothing that uses them moves ahead of it.
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
-                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
-                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :
-               : "memory");
+// Wait for columns asked for with tmem_ld.  The registers are named behind it, two at a time, so that nothing that uses them moves
+// ahead of the wait.
+template <int CH>
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[CH]) {
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < CH; i += 2) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]));
 }
 // acc += s * (NC columns of this thread's TMEM lane), CH columns on their way while CH are added.
 template <int NC, int CH>
@@ -86,26 +77,17 @@ __device__ __forceinline__ void promote(float2 (&acc)[NC / 2], uint32_t taddr, f
     }
   }
 }
-// The same with a factor per column: that of column c is lane c's `s` (columns 32 and on: lane c - 32's `s_hi`).
-template <int NC>
-__device__ __forceinline__ void promote_columns(float2 (&acc)[NC / 2], uint32_t taddr, float s, float s_hi) {
-  uint32_t r[2][16];
-  tmem_ld16(taddr, r[0]);
+// The same for 16 columns with a factor each, that of column c being lane c's `s`.
+__device__ __forceinline__ void promote_columns(float2 (&acc)[8], uint32_t taddr, float s) {
+  uint32_t r[16];
+  tmem_ld16(taddr, r);
+  float2 f[8];
 #pragma unroll
-  for (int c = 0; c < NC / 16; ++c) {
-    float2 f[8];
+  for (int i = 0; i < 8; ++i) f[i] = make_float2(__shfl_sync(0xFFFFFFFFu, s, 2 * i), __shfl_sync(0xFFFFFFFFu, s, 2 * i + 1));
+  tmem_wait(r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int col = c * 16 + 2 * i;
-      const float from = col < 32 ? s : s_hi;
-      f[i] = make_float2(__shfl_sync(0xFFFFFFFFu, from, col & 31), __shfl_sync(0xFFFFFFFFu, from, (col + 1) & 31));
-    }
-    tmem_wait(r[c & 1]);
-    if (c + 1 < NC / 16) tmem_ld16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      acc[c * 8 + i] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1])), f[i], acc[c * 8 + i]);
-  }
+  for (int i = 0; i < 8; ++i)
+    acc[i] = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f[i], acc[i]);
 }
 
 // The scales of A that a warp needs, R rows by the next 16 K blocks, in shared memory of its own.  A row's scales lie side by side
@@ -197,25 +179,42 @@ __device__ __forceinline__ uint32_t bf16x2(float2 f) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(f.x, f.y);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
-// 32 bytes of a row of `size`-byte elements from column n on, as far as the row goes.
+// 32 bytes of a row from column n on, as far as the row goes (it ends on a multiple of 16 bytes at least).
 template <typename T>
 __device__ __forceinline__ void store32(T* dst, const uint32_t (&w)[8], int n, int N, int vec) {
   constexpr int kPer = 32 / (int)sizeof(T);
   if (vec == 32) {
     if (n < N) st_global_v8(dst, w);
-  } else if (vec == 16) {
+  } else {
     if (n < N) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     if (n + kPer / 2 < N) *reinterpret_cast<uint4*>(dst + kPer / 2) = make_uint4(w[4], w[5], w[6], w[7]);
-  } else {
+  }
+}
+// A warp's 32 rows (from m0 on, one a lane) by NC columns where rows of C start anywhere: 32 columns at a time through shared memory
+// of the warp's own (32 x 33 floats), so that a store writes 32 columns of one row and not one column of 32 rows (1753 x 1001 x 1040:
+// XXX us so, YYY with a store per element).
+template <int NC, int OUT>
+__device__ __forceinline__ void store_ragged(const float2 (&acc)[NC / 2], const F8Gemm& g, int m0, int n0, float* s_rows, int lane) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (n + i < N) {
-        constexpr int kIn = 4 / (int)sizeof(T);
-        const uint32_t word = w[i / kIn] >> (8 * sizeof(T) * (i % kIn));
-        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[i] = word;
-        else if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)word;
-        else reinterpret_cast<uint8_t*>(dst)[i] = (uint8_t)word;
+  for (int c = 0; c < NC; c += 32) {
+    if (n0 + c >= g.N) break;                  // warp-uniform
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s_rows[lane * 33 + 2 * i] = acc[c / 2 + i].x;
+      s_rows[lane * 33 + 2 * i + 1] = acc[c / 2 + i].y;
+    }
+    __syncwarp();
+    const int n = n0 + c + lane;
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) {
+      const float v = s_rows[r * 33 + lane];
+      if (m0 + r < g.M && n < g.N) {
+        const long long at = (long long)(m0 + r) * g.N + n;
+        if constexpr (OUT == kOutBf16) static_cast<__nv_bfloat16*>(g.c)[at] = __float2bfloat16_rn(v);
+        else static_cast<float*>(g.c)[at] = v;
       }
+    }
   }
 }
 template <int NC, int OUT>
@@ -252,41 +251,37 @@ __device__ __forceinline__ void store_row(const float2 (&acc)[NC / 2], const F8G
     }
   }
 }
-// Finish and store NC columns of a row.  e4m3: the two warps that hold the halves of a block trade their maxima through `s_amax`
-// (two words a row) and `meet`, a barrier of theirs for two arrivals, `turn` the parity of its phase; the wait is bounded like every
-// other.
-template <int NC, int OUT>
-__device__ __forceinline__ void emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0) {
-  static_assert(NC == kF8Block, "a thread holds a whole block of an e4m3 result");
-  finish_row<NC, OUT>(acc, s_bias, g.act);
-  float inv = 0.f;
-  if constexpr (OUT == kOutF8) {
-    const F8Scale s = f8_scale(row_amax<NC>(acc));
-    inv = s.inv;
-    if (m < g.M && n0 < g.N) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
-  }
-  if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
+// A block's scale from its largest magnitude, and the factor for its values.
+__device__ __forceinline__ float put_scale(const F8Gemm& g, uint32_t amax, int m, int n0, bool mine) {
+  const F8Scale s = f8_scale(amax);
+  if (mine && m < g.M && n0 < g.N) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
+  return s.inv;
 }
+// Finish and store NC columns of a warp's 32 rows, m this lane's; s_rows: see store_ragged.  e4m3: the two warps that hold the halves
+// of a block trade their maxima through `s_amax` (two words a row) and `meet`, a barrier of theirs for two arrivals, used once; the
+// wait is bounded like every other (NC = 128 is a block by itself).
 template <int NC, int OUT>
-__device__ __forceinline__ bool emit_row(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, uint32_t* s_amax,
-                                         uint64_t* meet, uint32_t turn, int which, volatile int* abort_flag) {
+__device__ __forceinline__ void emit_rows(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, float* s_rows,
+                                          uint32_t* s_amax, uint64_t* meet, int which, volatile int* abort_flag) {
+  const int lane = threadIdx.x & 31;
   finish_row<NC, OUT>(acc, s_bias, g.act);
-  float inv = 0.f;
   if constexpr (OUT == kOutF8) {
-    static_assert(2 * NC == kF8Block, "two warps hold a block");
     uint32_t amax = row_amax<NC>(acc);
-    const int lane = threadIdx.x & 31;
-    s_amax[which * 32 + lane] = amax;
-    __syncwarp();
-    if (lane == 0) mbar_arrive(meet);
-    if (!mbar_wait_warp_inline(meet, turn, abort_flag)) return false;
-    amax = max(amax, s_amax[(which ^ 1) * 32 + lane]);
-    const F8Scale s = f8_scale(amax);
-    inv = s.inv;
-    if (m < g.M && n0 < g.N && which == 0) g.c_scale[(long long)m * ((g.N + kF8Block - 1) / kF8Block) + n0 / kF8Block] = s.scale;
+    if constexpr (NC < kF8Block) {
+      static_assert(2 * NC == kF8Block || OUT != kOutF8, "two warps hold a block");
+      s_amax[which * 32 + lane] = amax;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(meet);
+      if (!mbar_wait_warp(meet, 0, abort_flag)) return;
+      amax = max(amax, s_amax[(which ^ 1) * 32 + lane]);
+    }
+    const float inv = put_scale(g, amax, m, n0, which == 0);
+    if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
+  } else if (g.vec) {
+    if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, 0.f);
+  } else {
+    store_ragged<NC, OUT>(acc, g, m - lane, n0, s_rows, lane);
   }
-  if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
-  return true;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -299,11 +294,12 @@ __device__ __forceinline__ bool emit_row(float2 (&acc)[NC / 2], const F8Gemm& g,
 // ---------------------------------------------------------------------------------------------------------------
 template <int BN, bool SWAP>
 struct SplitCfg {
+  static_assert(!SWAP || BN == 16, "promote_columns");
   static constexpr int kWarps = SWAP ? 4 : 8;
   static constexpr int kThreads = 64 + 32 * kWarps;
   static constexpr int kCols = SWAP ? BN : BN / 2;             // of a warp
   static constexpr int kStageBytes = kRowBytes + BN * kStepK;
-  static constexpr int kStages = !SWAP ? (BN == 128 ? 4 : 5) : (BN == 16 ? 5 : (BN == 32 ? 4 : 3));
+  static constexpr int kStages = BN == 128 ? 4 : 5;
   static constexpr int kTmemCols = 2 * BN;                     // (a power of two, at least 32)
   static constexpr int kMaxSplit = SWAP ? 8 : 4;
   static constexpr size_t kBiasBytes = SWAP ? 0 : (size_t)kWarps * kCols * 4;
@@ -420,7 +416,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     constexpr int kWindow = Window::kBlocks;
     const Window window = {s_scale + (size_t)(warp - 2) * Window::kFloats, g.a_scale, g.M, k_blocks, lane};
     const float* sw = g.w_scale + (long long)(n0 / kF8Block) * k_blocks;
-    const int row0 = SWAP ? m0 : m0 + quad * 32, mine = SWAP && BN < 32 ? lane & (BN - 1) : lane;
+    const int row0 = SWAP ? m0 : m0 + quad * 32, mine = SWAP ? lane & (BN - 1) : lane;
     float w16 = 0.f, w16_next = 0.f;           // W's scales of a window, lane c that of block c
     auto fetch = [&](uint32_t w, int kb) {
       window.fetch(w, row0, kb, kb1);
@@ -435,13 +431,10 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         w16 = w16_next;
         fetch(w + 1, kb + kWindow);
       }
-      const float w_scale = __shfl_sync(0xFFFFFFFFu, w16, c);
-      const float f = window.at(w, c, mine) * w_scale;
-      float f_hi = 0.f;
-      if constexpr (SWAP && BN > 32) f_hi = window.at(w, c, 32 + lane) * w_scale;
+      const float f = window.at(w, c, mine) * __shfl_sync(0xFFFFFFFFu, w16, c);
       if (!(ok = mbar_wait_warp(&acc_full[buf], (j >> 1) & 1, abort_flag))) break;
       tc_fence_after();
-      if constexpr (SWAP) promote_columns<kCols>(acc, t_row + buf * BN, f, f_hi);
+      if constexpr (SWAP) promote_columns(acc, t_row + buf * BN, f);
       else promote<kCols, 16>(acc, t_row + buf * BN, f);
       tc_fence_before();
       __syncwarp();
@@ -505,7 +498,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   if (warp >= 2) {
     if constexpr (!SWAP) {
       if (owner == rank && ok)
-        ok = emit_row<kCols, OUT>(acc, g, s_bias, m0 + tile_row, n0 + half * kCols, s_amax + quad * 64, meet + quad, 0, half, abort_flag);
+        emit_rows<kCols, OUT>(acc, g, s_bias, m0 + tile_row, n0 + half * kCols, reinterpret_cast<float*>(smem) + (warp - 2) * 32 * 33,
+                              s_amax + quad * 64, meet + quad, half, abort_flag);      // (the operands' stages are free by now)
     } else {
       const int n = n0 + tile_row;
       const float b = g.bias != nullptr && n < g.N ? __bfloat162float(__ldg(g.bias + n)) : 0.f;
@@ -553,22 +547,22 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 // Persistent clusters of two CTAs, one per pair of SMs, on tiles of 256 x 256: each CTA fetches its own 128 rows of A and half
 // of the tile's rows of W, a K step of 128 costs an SM 32 KB from L2 for the 8.4 MFLOP it computes.
 //   warp 0       TMA producer (both CTAs, each its own operand rows; all bytes reported to the even CTA's barrier)
-//   warps 1, 2   MMA issuers (even CTA only), one for each half of the tile's columns: 4 x tcgen05.mma M256 N128 K32 per block
-//                into one of the half's two TMEM buffers; the commits free both CTAs' stage and hand the buffer to both CTAs
+//   warp 1       MMA issuer (even CTA only): 4 x tcgen05.mma M256 N256 K32 per block into one of two TMEM buffers; the commits free
+//                both CTAs' stage and hand the buffer to both CTAs' promotion
+//   warp 2       nothing
 //   warp 3       tensor memory; then the scales, 16 K blocks at a time
 //   warps 4..11  promotion and epilogue (both CTAs, each its own 128 rows): a warpgroup for each half of the columns
-// A buffer's round trip (MMAs, commit, promotion, hand-back through the other CTA's shared memory) is longer than a block's MMAs;
-// the halves have barriers of their own so that one half's MMAs run while the other half's buffers travel.
 // ---------------------------------------------------------------------------------------------------------------
 struct PairCfg {
   static constexpr int kBN = 256, kCols = 128;                 // of a tile, of a warp
   static constexpr int kWarps = 8, kThreads = 384;
   static constexpr int kStageBytes = kRowBytes + kBN / 2 * kStepK;
-  static constexpr int kStages = 6;                            // 192 KB
+  static constexpr int kStages = 5;                            // 160 KB
   static constexpr int kTmemCols = 512;
   static constexpr size_t kBiasBytes = (size_t)kWarps * kCols * 4;
   static constexpr size_t kScaleBytes = 2 * ScaleBlock::kFloats * 4;
-  static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kScaleBytes + kBarrierBytes;
+  static constexpr size_t kRowsBytes = (size_t)kWarps * 32 * 33 * 4;     // store_ragged
+  static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kScaleBytes + kRowsBytes + kBarrierBytes;
   // Registers: 384 threads start with 168 each; the first warpgroup gives up what the other two, with 128 sums a thread, take
   // (128 * 40 + 256 * 232 = 384 * 168).
   static constexpr int kFewRegs = 40, kManyRegs = 232;
@@ -587,12 +581,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
   float* s_scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
+  float* s_rows_all = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_rows_all) + Cfg::kRowsBytes);
   uint64_t* full = bars;                    // [kStages] both CTAs' TMA -> MMA (the even CTA's is the one in use)
-  uint64_t* empty = bars + kStages;         // [kStages] both issuers -> TMA (each CTA its own)
-  uint64_t* acc_full = bars + 2 * kStages;  // [half][2] MMA -> promotion (each CTA its own)
-  uint64_t* acc_empty = acc_full + 4;       // [half][2] both CTAs' promotion -> MMA (the even CTA's)
-  uint64_t* sc_full = acc_empty + 4;        // [2] scales -> promotion
+  uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA (each CTA its own)
+  uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion (each CTA its own)
+  uint64_t* acc_empty = acc_full + 2;       // [2] both CTAs' promotion -> MMA (the even CTA's)
+  uint64_t* sc_full = acc_empty + 2;        // [2] scales -> promotion
   uint64_t* sc_empty = sc_full + 2;         // [2] promotion -> scales
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -605,8 +600,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   const int k_blocks = (g.K - 1) / kStepK + 1;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
-    for (int i = 0; i < 4; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kWarps); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * Cfg::kWarps); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sc_full[i], 32); mbar_init(&sc_empty[i], Cfg::kWarps); }
     *abort_flag = 0;
     mbar_fence_init();
@@ -629,8 +624,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
       for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
         int mt, nt;
         tile_coords(tile, m_tiles, n_tiles, mt, nt);
-        // Of the 128 columns of a half the even CTA has the rows of W for the first 64, the odd one for the others.
-        const int row_a = (2 * mt + (int)rank) * kRows, row_w = nt * BN + (int)rank * (kCols / 2);
+        const int row_a = (2 * mt + (int)rank) * kRows, row_w = nt * BN + (int)rank * kCols;
         for (int kb = 0; kb < k_blocks; ++kb) {
           if (!(ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag))) break;
           // The even CTA's barrier counts the bytes of both CTAs.  The odd CTA's may land before it is armed: its
@@ -639,7 +633,6 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
           const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes), bar = cluster_map(smem_u32(&full[stage]), 0);
           tma_load_2d_pair(sa, &tm_a, bar, kb * kStepK, row_a);
           tma_load_2d_pair(sa + kRowBytes, &tm_w, bar, kb * kStepK, row_w);
-          tma_load_2d_pair(sa + kRowBytes + kRowBytes / 2, &tm_w, bar, kb * kStepK, row_w + kCols);
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -649,28 +642,27 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
         if (++stage == kStages) { stage = 0; phase ^= 1; }
       }
-    } else if ((warp == 1 || warp == 2) && rank == 0) {
-      // ------------------------------------------------------------ MMA issuers (even CTA)
+    } else if (warp == 1 && rank == 0) {
+      // ------------------------------------------------------------ MMA issuer (even CTA)
       const bool leader = elect_one();
-      const int half = warp - 1;
-      constexpr uint32_t idesc = idesc_e4m3(2 * kRows, BN / 2);
+      constexpr uint32_t idesc = idesc_e4m3(2 * kRows, BN);
       int stage = 0; uint32_t phase = 0;
       bool ok = true;
       uint32_t j = 0;                        // K blocks so far
       for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
         for (int kb = 0; kb < k_blocks; ++kb, ++j) {
           const uint32_t buf = j & 1;
-          if (!(ok = mbar_wait_warp_inline(&full[stage], phase, abort_flag))) break;
-          if (!(ok = mbar_wait_warp_inline(&acc_empty[2 * half + buf], ((j >> 1) & 1) ^ 1, abort_flag))) break;
+          if (!(ok = mbar_wait_warp(&full[stage], phase, abort_flag))) break;
+          if (!(ok = mbar_wait_warp(&acc_empty[buf], ((j >> 1) & 1) ^ 1, abort_flag))) break;
           tc_fence_after();
           const uint32_t sa = smem_u32(smem + (size_t)stage * Cfg::kStageBytes);
-          const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes + half * (kRowBytes / 2), 1024);
+          const uint64_t da = smem_desc_sw128(sa, 1024), db = smem_desc_sw128(sa + kRowBytes, 1024);
           if (leader) {
 #pragma unroll
             for (int k = 0; k < kStepK / 32; ++k)
-              mma_f8_ss_pair(tmem_base + (2 * half + buf) * kCols, da + 2 * k, db + 2 * k, idesc, k != 0);
+              mma_f8_ss_pair(tmem_base + buf * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
             mma_commit_pair(&empty[stage]);
-            mma_commit_pair(&acc_full[2 * half + buf]);
+            mma_commit_pair(&acc_full[buf]);
           }
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
@@ -696,8 +688,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     const int quad = warp & 3;                 // TMEM lane quadrant this warp may read
     const int half = (warp - 4) >> 2;          // which half of the tile's columns it has
     float* s_bias = s_bias_all + (size_t)(warp - 4) * kCols;
-    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 2 * kCols);
-    const uint32_t empty_bar = cluster_map(smem_u32(&acc_empty[2 * half]), 0);
+    const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
+    const uint32_t full_bar = smem_u32(acc_full), empty_bar = cluster_map(smem_u32(acc_empty), 0);
     uint32_t w = 0;                            // windows of scales so far
     bool ok = true;
     uint32_t j = 0;
@@ -725,18 +717,18 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
           __syncwarp();
           if (lane == 0) mbar_arrive(&sc_empty[(w - 1) & 1]);
         }
-        mbar_wait_lane(&sc_full[w & 1], (w >> 1) & 1, abort_flag);
+        mbar_wait_lane(smem_u32(&sc_full[w & 1]), (w >> 1) & 1, abort_flag);
         scales = s_scale + (w & 1) * ScaleBlock::kFloats;
         ++w;
       };
       turn();
       float a_next = scales[ScaleBlock::a_at(0, quad * 32 + lane)], w_next = scales[ScaleBlock::w_at(0, half)];
-      mbar_wait_lane(&acc_full[2 * half + (j & 1)], (j >> 1) & 1, abort_flag);
+      mbar_wait_lane(full_bar + (j & 1) * 8, (j >> 1) & 1, abort_flag);
       __syncwarp();
       tc_fence_after();
-      tmem_ld(t_row + (j & 1) * kCols, r[0]);
+      tmem_ld(t_row + (j & 1) * BN, r[0]);
       for (int kb = 0; kb < k_blocks; ++kb) {
-        const uint32_t taddr = t_row + (j & 1) * kCols;
+        const uint32_t taddr = t_row + (j & 1) * BN;
         const float f = a_next * w_next;
         const float2 s2 = make_float2(f, f);
         const bool more = kb + 1 < k_blocks;
@@ -755,12 +747,11 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster_relaxed(empty_bar + (j & 1) * 8);
             ++j;
-            if (more) {
-              mbar_wait_lane(&acc_full[2 * half + (j & 1)], (j >> 1) & 1, abort_flag);
-              __syncwarp();
-              tc_fence_after();
-              tmem_ld(t_row + (j & 1) * kCols, r[0]);
-            }
+            if (more) mbar_wait_lane(full_bar + (j & 1) * 8, (j >> 1) & 1, abort_flag);
+            __syncwarp();
+            tc_fence_after();
+            tmem_ld(t_row + (j & 1) * BN, r[0]);       // (behind the last block whatever is there: with a condition the 32
+                                                          // registers were copied from turn to turn)
           }
 #pragma unroll
           for (int i = 0; i < kPromote / 2; ++i) {
@@ -775,8 +766,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
           __syncwarp();
         }
       }
+      tmem_wait(r[0]);
       ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0);
-      if (ok) emit_row<kCols, OUT>(acc, g, s_bias, m, n_first);
+      if (ok) emit_rows<kCols, OUT>(acc, g, s_bias, m, n_first, s_rows_all + (warp - 4) * 32 * 33, nullptr, nullptr, 0, abort_flag);
     }
   }
 
@@ -820,13 +812,7 @@ int launch_split(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm&
 template <int OUT>
 int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
   if (plan.split == 0) return launch_pair<OUT>(tm_a, tm_w, g, d_status, s);
-  if (plan.swap) {
-    switch (plan.bn) {
-      case 16: return launch_split<16, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
-      case 32: return launch_split<32, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
-      default: return launch_split<64, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
-    }
-  }
+  if (plan.swap) return launch_split<16, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
   if constexpr (OUT != kOutF8)
     if (plan.bn == 64) return launch_split<64, false, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
   return launch_split<128, false, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
@@ -842,10 +828,7 @@ TcGemmF8Plan plan_tc_gemm_fp8(int M, int Nout, int K, bool f8_out, int sms) {
     while (split * 2 <= most && split * 2 <= kb && tiles * split * 2 <= room) split *= 2;
     return split;
   };
-  if (M <= 64) {
-    const int bn = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
-    return {bn, spread(ceil_div(Nout, kRows), 2 * sms, 8), true};
-  }
+  if (M <= 48) return {16, spread(ceil_div(Nout, kRows) * ceil_div(M, 16), 2 * sms, 8), true};
   if (ceil_div(M, 256) * ceil_div(Nout, 256) >= 60) return {256, 0, false};
   const long long tiles = ceil_div(M, kRows) * ceil_div(Nout, 128);
   return {128, spread(tiles, sms, 4), false};
@@ -856,7 +839,7 @@ int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const
   const TcGemmF8Plan plan = plan_tc_gemm_fp8(M, Nout, K, out_dtype == HERO_DTYPE_E4M3, num_sms());
   CUtensorMap tm_a, tm_w;
   HERO_TRY(make_tmap_bytes(&tm_a, a, (uint64_t)M, (uint64_t)K, plan.swap ? plan.bn : kRows));
-  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? PairCfg::kCols / 2 : (plan.swap ? kRows : plan.bn)));
+  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? PairCfg::kCols : (plan.swap ? kRows : plan.bn)));
   F8Gemm g = {a_scale, w_scale, static_cast<const __nv_bfloat16*>(bias), c, c_scale, M, Nout, K, act, 0};
   const unsigned long long low = (unsigned long long)reinterpret_cast<uintptr_t>(c) |
                                  (unsigned long long)Nout * (out_dtype == HERO_DTYPE_FP32 ? 4 : (out_dtype == HERO_DTYPE_BF16 ? 2 : 1));
