@@ -820,18 +820,52 @@ int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensor
 
 }  // namespace
 
+// ---------------------------------------------------------------------------------------------------------------
+// Which kernel, which tile, how many CTAs per tile.  The estimate is in nanoseconds: rounds of tiles times (K blocks times the
+// time of a block, plus what a tile costs besides) plus what a launch costs, and for a split tile the exchange.  Fitted to 127
+// problems (1 to 3510 rows, 256 to 12288 columns, K 512 to 12288), each timed with every kernel in launches in a row; on them
+// the rule's choice takes 0.3 % longer than the best on average and 12 % at worst.  Some of them (us; 16 exchanged over 1 / 2 / 4,
+// 128 over 1 / 2 / 4, 64 over 1 / 2 / 4, pair):
+//   1 x 12288 x 3072     10.7 / 10.6 / 16.5 | 17.3 / 21.1 / 27.9 | 24.0 / 28.1 / 43.5 | 18.0
+//   1 x 3072 x 12288     30.2 / 17.7 / 12.4 | 40.2 / 23.1 / 15.8 | 35.0 / 24.2 / 25.1 | 41.8
+//   16 x 2304 x 768      4.3 / 4.5 / 5.1 | 4.8 / 5.1 / 6.0 | 4.3 / 4.2 / 8.9 | 6.3
+//   48 x 12288 x 3072    11.8 / 20.0 / 39.4 | 13.2 / 19.1 / 25.9 | 21.8 / 23.9 / 39.6 | 15.6
+//   64 x 3072 x 3072     10.3 / 8.8 / 15.1 | 12.5 / 9.3 / 8.4 | 11.2 / 8.0 / 12.8 | 14.6
+//   200 x 1280 x 5120    - / - / - | 18.9 / 12.4 / 9.8 | 16.5 / 10.7 / 15.0 | 21.6
+//   614 x 3072 x 3072    - / - / - | 13.1 / 19.3 / 33.5 | 21.8 / 31.7 / 51.8 | 15.8
+//   1394 x 3072 x 3072   - / - / - | 25.7 / 38.7 / 68.2 | 43.3 / 63.0 / 107.7 | 16.7
+//   1394 x 2304 x 768    - / - / - | 11.4 / 18.9 / 40.7 | 14.5 / 30.5 / 63.2 | 9.2
+//   3510 x 768 x 3072    - / - / - | 25.2 / 28.4 / 48.1 | 32.1 / 39.5 / 70.2 | 16.7
+// ---------------------------------------------------------------------------------------------------------------
 TcGemmF8Plan plan_tc_gemm_fp8(int M, int Nout, int K, bool f8_out, int sms) {
   const long long kb = ((long long)K + kStepK - 1) / kStepK;
   auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
-  auto spread = [&](long long tiles, long long room, int most) {
-    int split = 1;
-    while (split * 2 <= most && split * 2 <= kb && tiles * split * 2 <= room) split *= 2;
-    return split;
+  TcGemmF8Plan best = {PairCfg::kBN, 0, false};
+  const long long pairs = sms < 2 ? 1 : sms / 2;
+  long long best_t = ceil_div(ceil_div(M, 2 * kRows) * ceil_div(Nout, PairCfg::kBN), pairs) * (kb * 500 + 2420) + 1230;
+  auto consider = [&](int bn, int split, bool swap, long long t) {
+    if (t < best_t) { best_t = t; best = {bn, split, swap}; }
   };
-  if (M <= 48) return {16, spread(ceil_div(Nout, kRows) * ceil_div(M, 16), 2 * sms, 8), true};
-  if (ceil_div(M, 256) * ceil_div(Nout, 256) >= 60) return {256, 0, false};
-  const long long tiles = ceil_div(M, kRows) * ceil_div(Nout, 128);
-  return {128, spread(tiles, sms, 4), false};
+  for (int split = 1; split <= 8 && split <= kb; split *= 2) {     // two CTAs an SM; the weights' bandwidth is shared by all
+    const long long ctas = ceil_div(Nout, kRows) * ceil_div(M, 16) * split, room = 2ll * sms;
+    if (ctas > 0x7FFFFFFFll) break;
+    const long long shared = 19 * (ctas < room ? ctas : room) / 10, exchange = split == 1 ? 0 : 763 + 366 * (split - 2) + 9 * ctas;
+    consider(16, split, true, ceil_div(ctas, room) * (ceil_div(kb, split) * (shared > 263 ? shared : 263) + 214) + 2440 + exchange);
+  }
+  struct { int bn, step, step_full, tile, launch, two, four, crowd; } const one[] = {{128, 337, 184, 1393, 1451, 1468, 2117, 1194},
+                                                                                      {64, 227, 204, 770, 2070, 810, 948, 975}};
+  for (const auto& o : one) {
+    if (f8_out && o.bn < kF8Block) continue;           // (an e4m3 result's blocks of 128 columns stay in one tile)
+    for (int split = 1; split <= 4 && split <= kb; split *= 2) {
+      const long long ctas = ceil_div(M, kRows) * ceil_div(Nout, o.bn) * split;
+      if (ctas > 0x7FFFFFFFll) break;
+      // (clusters of four do not fill the chip: they need four free SMs of one processing cluster)
+      const long long room = split < 4 ? sms : (sms < 8 ? sms : sms * 7 / 8), step = o.step + o.step_full * (ctas < sms ? ctas : sms) / sms;
+      const long long exchange = split == 1 ? 0 : (split == 2 ? o.two : o.four + (ctas > 60 ? o.crowd * (ctas - 60) / 60 : 0));
+      consider(o.bn, split, false, ceil_div(ctas, room) * (ceil_div(kb, split) * step + o.tile) + o.launch + exchange);
+    }
+  }
+  return best;
 }
 
 int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const void* bias, void* c,
