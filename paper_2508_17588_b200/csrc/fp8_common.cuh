@@ -14,7 +14,6 @@ namespace hero {
 constexpr int kF8Block = 128;                    // columns (and, for weights, rows) of a block
 constexpr float kF8InvMax = 1.0f / 448.0f;
 constexpr float kF8ScaleFloor = 1.17549435e-38f; // 2^-126
-constexpr uint32_t kFiniteMax = 0x7F7FFFFFu;     // bits of the largest finite fp32
 
 // Magnitudes as their bits: ordered like the numbers, infinity above every number and NaN above infinity, so that an integer
 // maximum carries both through.
@@ -25,7 +24,7 @@ __device__ __forceinline__ F8Scale f8_scale(uint32_t amax_bits) {
   F8Scale r;
   r.scale = fmaxf(__uint_as_float(amax_bits) * kF8InvMax, kF8ScaleFloor);
   r.inv = 1.0f / r.scale;
-  if (amax_bits > kFiniteMax) r.scale = r.inv = __uint_as_float(0x7FC00000u);
+  if (amax_bits > 0x7F7FFFFFu) r.scale = r.inv = __uint_as_float(0x7FC00000u);
   return r;
 }
 // Four values to four e4m3 bytes, the first in the lowest.  (|v| is at most 448 and a rounding: nothing saturates.)

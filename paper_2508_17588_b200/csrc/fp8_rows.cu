@@ -1,6 +1,7 @@
 // Kernels that write 8-bit operands with a scale per block, and the root-mean-square norm: one pass over the data each,
 // bound by HBM.
 //
+//  * gather_ln_f8_kernel: the refresh prologue (gather, LayerNorm, modulation) in e4m3 with a scale per 128 columns.
 //  * rms_norm_kernel: h = x + add (kept in the run dtype if asked for), y = h / sqrt(mean(h^2) + eps) * gain, y in the run dtype or
 //    in e4m3 with a scale per 128 columns.
 //  * quantize_rows_kernel / quantize_tiles_kernel: a matrix to e4m3 with a scale per 1 x 128 or 128 x 128 elements.
@@ -10,7 +11,7 @@
 namespace hero {
 namespace {
 
-// ------------------------------------------------------------------ 16-byte packets
+// ------------------------------------------------------------------ 16 bytes of a lane
 template <typename T>
 struct Pack;
 template <>
@@ -45,160 +46,425 @@ struct Pack<__nv_bfloat16> {
   }
 };
 
-// The lanes that hold a block's 128 columns: 16 of bf16 packets, 32 of fp32 ones.
 template <typename T>
-__device__ __forceinline__ uint32_t block_amax(const float (&f)[Pack<T>::N]) {
+__device__ __forceinline__ void store_f8(uint8_t* q, const float (&f)[Pack<T>::N], float inv) {      // (q: where the packet goes)
+  const uint32_t a = f8_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+  if constexpr (Pack<T>::N == 8) __stcs(reinterpret_cast<uint2*>(q), make_uint2(a, f8_pack4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)));
+  else __stcs(reinterpret_cast<unsigned int*>(q), a);
+}
+
+// Scales of a row's blocks from the magnitudes' bits m[c] that a lane has in its chunk c of 32 lanes (zeros past the end of the row), blocks
+// being LANES lanes that stand side by side: factors for the lane's values, scales to `row_scale`.  The maxima of all chunks go through
+// the shuffles together, and of a block's lanes each works out another chunk's scale, so that a warp divides once a row and not
+// once a chunk.  v0: place of the lane's chunk 0 in the row, step: from a chunk to the next, n: places in the row.
+template <int LANES, int V>
+__device__ __forceinline__ void row_scales(uint32_t (&m)[V], float (&inv)[V], float* row_scale, int v0, int step, int n) {
+  static_assert(V <= LANES, "a lane for every chunk of a block");
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int c = 0; c < V; ++c) m[c] = max(m[c], __shfl_xor_sync(0xFFFFFFFFu, m[c], o));
+  const int lane = threadIdx.x & 31, mine = lane & (LANES - 1);
+  uint32_t pick = m[0];
+#pragma unroll
+  for (int c = 1; c < V; ++c) pick = mine == c ? m[c] : pick;
+  const F8Scale s = f8_scale(pick);
+  const int first = v0 - mine + mine * step;           // first place of the block that this lane did
+  if (mine < V && first < n) row_scale[first / LANES] = s.scale;
+#pragma unroll
+  for (int c = 0; c < V; ++c) inv[c] = V == 1 ? s.inv : __shfl_sync(0xFFFFFFFFu, s.inv, (lane & ~(LANES - 1)) | c);
+}
+
+// ------------------------------------------------------------------ 32 bytes of a lane
+// A lane's piece of a row: two packets of 16 bytes, N elements as pairs; kLanes of them are a block of 128 columns.
+template <typename T>
+struct Piece {
+  static constexpr int N = 32 / (int)sizeof(T), kLanes = kF8Block / N, kPacket = N / 2;
+};
+__device__ __forceinline__ void unpack(const uint4 (&r)[2], float2 (&f)[4], float) {
+  f[0] = make_float2(__uint_as_float(r[0].x), __uint_as_float(r[0].y)); f[1] = make_float2(__uint_as_float(r[0].z), __uint_as_float(r[0].w));
+  f[2] = make_float2(__uint_as_float(r[1].x), __uint_as_float(r[1].y)); f[3] = make_float2(__uint_as_float(r[1].z), __uint_as_float(r[1].w));
+}
+__device__ __forceinline__ void unpack(const uint4 (&r)[2], float2 (&f)[8], __nv_bfloat16) {
+  const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ void pack(uint4 (&r)[2], const float2 (&f)[4], float) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    r[h] = make_uint4(__float_as_uint(f[2 * h].x), __float_as_uint(f[2 * h].y), __float_as_uint(f[2 * h + 1].x), __float_as_uint(f[2 * h + 1].y));
+}
+__device__ __forceinline__ void pack(uint4 (&r)[2], const float2 (&f)[8], __nv_bfloat16) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(f[i].x, f[i].y);
+    w[i] = *reinterpret_cast<const uint32_t*>(&p);
+  }
+  r[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  r[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+// Packets 2v and 2v + 1 of a row that has `packets` (zeros past its end).
+template <bool STREAM>
+__device__ __forceinline__ void load_piece(uint4 (&r)[2], const void* row, int v, int packets) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint4* from = static_cast<const uint4*>(row) + 2 * v + h;
+    r[h] = 2 * v + h < packets ? (STREAM ? __ldcs(from) : __ldg(from)) : make_uint4(0, 0, 0, 0);
+  }
+}
+__device__ __forceinline__ void store_piece(void* row, const uint4 (&r)[2], int v, int packets) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (2 * v + h < packets) __stcs(static_cast<uint4*>(row) + 2 * v + h, r[h]);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t piece_amax(const float2 (&f)[Piece<T>::N / 2]) {
   uint32_t m = 0;
 #pragma unroll
-  for (int q = 0; q < Pack<T>::N; ++q) m = max(m, abs_bits(f[q]));
-#pragma unroll
-  for (int o = kF8Block / Pack<T>::N / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  for (int i = 0; i < Piece<T>::N / 2; ++i) m = max(max(m, abs_bits(f[i].x)), abs_bits(f[i].y));
   return m;
 }
-// A packet's worth of e4m3 to `q` (N bytes).
+// Piece v of a row to e4m3 (`row`: the row's bytes).
 template <typename T>
-__device__ __forceinline__ void store_f8(uint8_t* q, const float (&f)[Pack<T>::N], float inv) {
-  const uint32_t a = f8_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-  if constexpr (Pack<T>::N == 8) {
-    const uint32_t b = f8_pack4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
-    __stcs(reinterpret_cast<uint2*>(q), make_uint2(a, b));
-  } else {
-    __stcs(reinterpret_cast<unsigned int*>(q), a);
+__device__ __forceinline__ void store_f8(uint8_t* row, const float2 (&f)[Piece<T>::N / 2], float inv, int v) {
+  constexpr int N = Piece<T>::N;
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float2 a = __fmul2_rn(f[2 * i], make_float2(inv, inv)), b = __fmul2_rn(f[2 * i + 1], make_float2(inv, inv));
+    w[i] = f8_pack4(a.x, a.y, b.x, b.y);
+  }
+  if constexpr (N == 16) __stcs(reinterpret_cast<uint4*>(row) + v, make_uint4(w[0], w[1], w[2], w[3]));
+  else __stcs(reinterpret_cast<uint2*>(row) + v, make_uint2(w[0], w[1]));
+}
+
+// ------------------------------------------------------------------ rows in registers
+// G warps hold a row, V pieces a lane (the last predicated), G growing with the row so that a lane never holds more than three: all
+// its loads are in flight at once, and enough rows are resident.  One row and done: CTAs that stay and fetch the next row ahead took
+// 122 us for 35552 rows of 3072 where these take 114.  Beside the bytes the kernel costs instructions, about as long as the bytes where a
+// row is read once and written in 8 bits: 8774 rows of 3072 bf16 through the norm alone take 16.3 us with packed arithmetic, a scale
+// a warp and no division by the row's length, 20.4 without.
+__host__ __device__ constexpr int rows_threads(int g) { return g == 1 ? 256 : 32 * g; }
+template <int G>
+struct RowThreads {
+  int lane, warp, t;             // t: among the row's threads
+  long long row;
+  __device__ __forceinline__ RowThreads()
+      : lane(threadIdx.x & 31), warp(threadIdx.x >> 5), t(G == 1 ? threadIdx.x & 31 : threadIdx.x),
+        row(G == 1 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x) {}
+  // Sum over a row; `part` [G] is used once.
+  __device__ __forceinline__ float total(float v, float* part) const {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if constexpr (G > 1) {
+      if (lane == 0) part[warp] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < G; ++w) v += part[w];
+    }
+    return v;
+  }
+};
+// x, and add where there is one, as fp32 pairs.
+template <typename T, int G, int V>
+__device__ __forceinline__ void load_rows(float2 (&f)[V][Piece<T>::N / 2], const T* x, const T* add, int t, int packets) {
+  uint4 vx[V][2], va[V][2];
+#pragma unroll
+  for (int c = 0; c < V; ++c) load_piece<true>(vx[c], x, c * 32 * G + t, packets);
+  if (add) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) load_piece<true>(va[c], add, c * 32 * G + t, packets);
+  }
+#pragma unroll
+  for (int c = 0; c < V; ++c) {
+    unpack(vx[c], f[c], T());
+    if (add) {
+      float2 g[Piece<T>::N / 2];
+      unpack(va[c], g, T());
+#pragma unroll
+      for (int i = 0; i < Piece<T>::N / 2; ++i) f[c][i] = __fadd2_rn(f[c][i], g[i]);
+    }
   }
 }
 
 // ------------------------------------------------------------------ root-mean-square norm
-// G warps hold a row in registers, VPL packets of 16 bytes a lane (the last predicated): x and add are read once, the sum of
-// squares is reduced by shuffles (and, over several warps, through shared memory), everything is written from the registers.
-// G grows with the row so that a lane never holds more than six packets and all its loads are in flight at once.
-// A thread reads and writes the same packets, so `sum` may be x or add.
-constexpr int rms_threads(int g) { return g == 1 ? 256 : 32 * g; }
-template <typename T, int G, int VPL, bool Q8>
-__global__ void __launch_bounds__(rms_threads(G))
+// A thread reads and writes the same packets of a row, so `sum` (or, in the run dtype, `out`) may be x or add.
+// Bound by HBM: 35552 x 3072 bf16 with add and sum, e4m3 out, 114 us (6.7 TB/s).
+template <typename T, int G, int V, bool Q8>
+__global__ void __launch_bounds__(rows_threads(G))
 rms_norm_kernel(const T* x, const T* add, const T* __restrict__ gain, T* sum, void* out, float* __restrict__ out_scale,
-                int rows, int D, float eps) {
+                int rows, int D, float inv_d, float eps) {
   stream_order();
-  using P = Pack<T>;
-  constexpr int kRows = G == 1 ? 8 : 1;
-  __shared__ float s_part[G == 1 ? 1 : G];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long row = (long long)blockIdx.x * kRows + (G == 1 ? warp : 0);
-  if (G == 1 && row >= rows) return;
-  const int t = G == 1 ? lane : (int)threadIdx.x;
-  const int packets = D / P::N;
-  const uint4* xr = reinterpret_cast<const uint4*>(x + row * D);
-  const uint4* ar = reinterpret_cast<const uint4*>(add + row * D);
-  uint4 vx[VPL], va[VPL];
+  constexpr int N = Piece<T>::N;
+  __shared__ float s_part[G];
+  const RowThreads<G> w;
+  if (G == 1 && w.row >= rows) return;
+  const int packets = D / Piece<T>::kPacket;
+  const long long at = w.row * D;
+  float2 f[V][N / 2];
+  load_rows<T, G, V>(f, x + at, add ? add + at : nullptr, w.t, packets);
+  float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int c = 0; c < VPL; ++c) {
-    const int v = c * 32 * G + t;
-    vx[c] = va[c] = make_uint4(0, 0, 0, 0);
-    if (v < packets) {
-      vx[c] = __ldcs(xr + v);
-      if (add) va[c] = __ldcs(ar + v);
+  for (int c = 0; c < V; ++c) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) sq = __ffma2_rn(f[c][i], f[c][i], sq);
+    if (sum) {
+      uint4 r[2];
+      pack(r, f[c], T());
+      store_piece(sum + at, r, c * 32 * G + w.t, packets);
     }
   }
-  float f[VPL][P::N];
-  float sq = 0.f;
+  const float rstd = rsqrtf(fmaf(w.total(sq.x + sq.y, s_part), inv_d, eps));
+  uint32_t m[V];
 #pragma unroll
-  for (int c = 0; c < VPL; ++c) {
-    P::unpack(vx[c], f[c]);
-    if (add) {
-      float g[P::N];
-      P::unpack(va[c], g);
+  for (int c = 0; c < V; ++c) {
+    const int v = c * 32 * G + w.t;
 #pragma unroll
-      for (int q = 0; q < P::N; ++q) f[c][q] += g[q];
-    }
+    for (int i = 0; i < N / 2; ++i) f[c][i] = __fmul2_rn(f[c][i], make_float2(rstd, rstd));
+    if (gain) {
+      uint4 r[2];
+      float2 g[N / 2];
+      load_piece<false>(r, gain, v, packets);
+      unpack(r, g, T());
 #pragma unroll
-    for (int q = 0; q < P::N; ++q) sq = fmaf(f[c][q], f[c][q], sq);
-    const int v = c * 32 * G + t;
-    if (sum && v < packets) __stcs(reinterpret_cast<uint4*>(sum + row * D) + v, P::pack(f[c]));
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
-  if constexpr (G > 1) {
-    if (lane == 0) s_part[warp] = sq;
-    __syncthreads();
-    sq = 0.f;
-#pragma unroll
-    for (int w = 0; w < G; ++w) sq += s_part[w];
-  }
-  const float rstd = 1.0f / sqrtf(sq / (float)D + eps);
-#pragma unroll
-  for (int c = 0; c < VPL; ++c) {
-    const int v = c * 32 * G + t;
-#pragma unroll
-    for (int q = 0; q < P::N; ++q) f[c][q] *= rstd;
-    if (gain && v < packets) {
-      float g[P::N];
-      P::unpack(__ldg(reinterpret_cast<const uint4*>(gain) + v), g);
-#pragma unroll
-      for (int q = 0; q < P::N; ++q) f[c][q] *= g[q];
+      for (int i = 0; i < N / 2; ++i) f[c][i] = __fmul2_rn(f[c][i], g[i]);
     }
     if constexpr (Q8) {
-      constexpr int kLanes = kF8Block / P::N;        // lanes of a block
-      const F8Scale s = f8_scale(block_amax<T>(f[c]));
-      if (v < packets) {
-        store_f8<T>(static_cast<uint8_t*>(out) + row * D + (long long)v * P::N, f[c], s.inv);
-        if (v % kLanes == 0) out_scale[row * ((D + kF8Block - 1) / kF8Block) + v / kLanes] = s.scale;
-      }
-    } else if (v < packets) {
-      __stcs(reinterpret_cast<uint4*>(static_cast<T*>(out) + row * D) + v, P::pack(f[c]));
+      m[c] = piece_amax<T>(f[c]);
+    } else {
+      uint4 r[2];
+      pack(r, f[c], T());
+      store_piece(static_cast<T*>(out) + at, r, v, packets);
     }
   }
+  if constexpr (Q8) {
+    float inv[V];
+    row_scales<Piece<T>::kLanes, V>(m, inv, out_scale + w.row * ((D + kF8Block - 1) / kF8Block), w.t, 32 * G, packets / 2);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const int v = c * 32 * G + w.t;
+      if (2 * v < packets) store_f8<T>(static_cast<uint8_t*>(out) + at, f[c], inv[c], v);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ gather + LayerNorm + modulate
+// G warps take the rows of ONE batch item one after the other, a lane V packets of 16 bytes of each, and with them the item's
+// (1 + scale) and shift of those columns: a thread puts the ones that it needs into shared memory, side by side with its neighbours'
+// (no bank conflicts, and nobody else reads them, so no barrier).  The vectors are twice as long as a bf16 row; 8774 rows of 3072 with a
+// second row to add took 33 us with the vectors read from L1 for every row, 39 with them in registers, which leaves 12 warps an SM, and
+// 32 so.  The next row is on its way while this one is reduced (mean, then squared differences from it) and stored.
+__host__ __device__ constexpr int ln_threads(int g) { return g == 1 ? 256 : 32 * g; }
+constexpr int ln_smem(int g, int v, int n) { return v * 2 * n * 4 * ln_threads(g); }
+constexpr int ln_ctas_per_sm(int g, int v, int n) {            // n elements a packet; registers: the row and the next two packets
+  const int regs = 40 + v * (n + 8), warps = ln_threads(g) / 32, by_regs = 64 * 1024 / (32 * warps * ((regs + 7) / 8 * 8));
+  const int by_smem = 220 * 1024 / (ln_smem(g, v, n) + 1024), by_warps = 64 / warps;
+  const int least = by_regs < by_smem ? (by_regs < by_warps ? by_regs : by_warps) : (by_smem < by_warps ? by_smem : by_warps);
+  return least < 1 ? 1 : least;
+}
+template <typename T, int G, int V>
+__global__ void __launch_bounds__(ln_threads(G), ln_ctas_per_sm(G, V, Pack<T>::N))
+gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const int* __restrict__ idx, const float* __restrict__ shift,
+                    const float* __restrict__ scale, int mod_ld, int vec, uint8_t* __restrict__ out, float* __restrict__ out_scale,
+                    int n_rows, int n_sel, int B, int D, float inv_d, float eps) {
+  stream_order();
+  using P = Pack<T>;
+  constexpr int N = P::N, kLanes = kF8Block / N, kThreads = ln_threads(G);
+  extern __shared__ float4 s_mod[];              // [V][1 + scale, shift][N / 4][threads]
+  __shared__ float s_part[2][G];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = G == 1 ? lane : (int)threadIdx.x;
+  const int b = blockIdx.x % B, packets = D / N, blocks = (D + kF8Block - 1) / kF8Block;
+  const long long first = G == 1 ? (long long)(blockIdx.x / B) * 8 + warp : blockIdx.x / B, step = (long long)(gridDim.x / B) * (G == 1 ? 8 : 1);
+  uint4 vx[V], va[V];
+  long long listed = 0;                          // row of x for the row after the fetched one
+  auto look = [&](long long i) {
+    if (i < n_sel) listed = (long long)b * n_rows + (idx ? __ldg(idx + i) : i);
+  };
+  auto fetch = [&](long long i) {                // (look(i) came before)
+    if (i >= n_sel) return;
+    const uint4* xr = reinterpret_cast<const uint4*>(x + listed * D);
+    const uint4* ar = reinterpret_cast<const uint4*>(add + listed * D);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const int v = c * 32 * G + t;
+      vx[c] = v < packets ? __ldcs(xr + v) : make_uint4(0, 0, 0, 0);
+      if (add) va[c] = v < packets ? __ldcs(ar + v) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto total = [&](float2 p, float* part) {      // over the row
+    float v = p.x + p.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if constexpr (G > 1) {
+      if (lane == 0) part[warp] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < G; ++w) v += part[w];
+    }
+    return v;
+  };
+  look(first);
+  fetch(first);
+  look(first + step);
+  const float* sc = scale + (long long)b * mod_ld;
+  const float* sh = shift + (long long)b * mod_ld;
+#pragma unroll
+  for (int c = 0; c < V; ++c) {
+    const int v = c * 32 * G + t;
+    if (v < packets) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) {
+        float4 s4, h4;
+        if (vec) {
+          s4 = __ldg(reinterpret_cast<const float4*>(sc) + v * (N / 4) + q);
+          h4 = __ldg(reinterpret_cast<const float4*>(sh) + v * (N / 4) + q);
+        } else {
+          const float *a = sc + v * N + 4 * q, *e = sh + v * N + 4 * q;
+          s4 = make_float4(__ldg(a), __ldg(a + 1), __ldg(a + 2), __ldg(a + 3));
+          h4 = make_float4(__ldg(e), __ldg(e + 1), __ldg(e + 2), __ldg(e + 3));
+        }
+        s_mod[((c * 2) * (N / 4) + q) * kThreads + threadIdx.x] = make_float4(1.0f + s4.x, 1.0f + s4.y, 1.0f + s4.z, 1.0f + s4.w);
+        s_mod[((c * 2 + 1) * (N / 4) + q) * kThreads + threadIdx.x] = h4;
+      }
+    }
+  }
+  for (long long i = first; i < n_sel; i += step) {            // (the same turns for a row's threads)
+    float2 f[V][N / 2];
+    float2 sum = make_float2(0.f, 0.f), sq = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      P::unpack(vx[c], reinterpret_cast<float(&)[N]>(f[c]));
+      if (add) {
+        float2 a[N / 2];
+        P::unpack(va[c], reinterpret_cast<float(&)[N]>(a));
+#pragma unroll
+        for (int q = 0; q < N / 2; ++q) f[c][q] = __fadd2_rn(f[c][q], a[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < N / 2; ++q) sum = __fadd2_rn(sum, f[c][q]);
+    }
+    fetch(i + step);
+    look(i + 2 * step);
+    const float mean = total(sum, s_part[0]) * inv_d;
+#pragma unroll
+    for (int c = 0; c < V; ++c)
+      if (c * 32 * G + t < packets) {            // (absent packets stay zeros)
+#pragma unroll
+        for (int q = 0; q < N / 2; ++q) {
+          f[c][q] = __fadd2_rn(f[c][q], make_float2(-mean, -mean));
+          sq = __ffma2_rn(f[c][q], f[c][q], sq);
+        }
+      }
+    const float rstd = rsqrtf(fmaf(total(sq, s_part[1]), inv_d, eps));
+    uint32_t m[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      m[c] = 0;
+      if (c * 32 * G + t < packets) {
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) {
+          const float4 s4 = s_mod[((c * 2) * (N / 4) + q) * kThreads + threadIdx.x], h4 = s_mod[((c * 2 + 1) * (N / 4) + q) * kThreads + threadIdx.x];
+          float2 &u = f[c][2 * q], &w = f[c][2 * q + 1];
+          u = __ffma2_rn(__fmul2_rn(u, make_float2(rstd, rstd)), make_float2(s4.x, s4.y), make_float2(h4.x, h4.y));
+          w = __ffma2_rn(__fmul2_rn(w, make_float2(rstd, rstd)), make_float2(s4.z, s4.w), make_float2(h4.z, h4.w));
+          m[c] = max(max(m[c], max(abs_bits(u.x), abs_bits(u.y))), max(abs_bits(w.x), abs_bits(w.y)));
+        }
+      }
+    }
+    const long long row = (long long)b * n_sel + i;
+    float inv[V];
+    row_scales<kLanes, V>(m, inv, out_scale + row * blocks, t, 32 * G, packets);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const int v = c * 32 * G + t;
+      if (v < packets) store_f8<T>(out + row * D + (long long)v * N, reinterpret_cast<const float(&)[N]>(f[c]), inv[c]);
+    }
+  }
+}
+
+// The smallest G warps a row and V pieces (or packets) a lane that hold a row of `chunks` times 32 of them.
+#define HERO_ROWS_CASE(G, V, LAUNCH) \
+  if (chunks <= G * V) { LAUNCH(G, V); }
+#define HERO_ROWS(LAUNCH)                                                              \
+  HERO_ROWS_CASE(1, 1, LAUNCH) HERO_ROWS_CASE(1, 2, LAUNCH) HERO_ROWS_CASE(1, 3, LAUNCH)  \
+  HERO_ROWS_CASE(2, 2, LAUNCH) HERO_ROWS_CASE(2, 3, LAUNCH)                              \
+  HERO_ROWS_CASE(4, 2, LAUNCH) HERO_ROWS_CASE(4, 3, LAUNCH)                              \
+  HERO_ROWS_CASE(8, 2, LAUNCH) HERO_ROWS_CASE(8, 3, LAUNCH)                              \
+  HERO_ROWS_CASE(16, 2, LAUNCH) HERO_ROWS_CASE(16, 3, LAUNCH)
+static inline int row_chunks(int D, int piece) { return (D + 32 * piece - 1) / (32 * piece); }
+static inline long long row_ctas(int g, long long rows) { return g == 1 ? (rows + 7) / 8 : rows; }
+
+template <typename T>
+int gather_ln_f8_dispatch(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld, void* out,
+                          float* out_scale, int B, int N, int n_sel, int D, float eps, cudaStream_t s) {
+  const int chunks = row_chunks(D, Pack<T>::N);
+  const int vec = mod_ld % 4 == 0 && aligned16(shift) && aligned16(scale);       // the vectors may be read 16 bytes at a time
+  // the same number of CTAs for every batch item, at most as many as stay resident
+  auto ctas = [&](int g, int per_sm) {
+    const int need = g == 1 ? (n_sel - 1) / 8 + 1 : n_sel, most = (num_sms() * per_sm + B - 1) / B;
+    return (unsigned)((need < most ? need : most) * B);
+  };
+#define HERO_LN_F8(G, V)                                                                                                              \
+  constexpr int smem = ln_smem(G, V, Pack<T>::N);                                                                                     \
+  if (smem > 47 * 1024) {                                                                                                             \
+    static PerDeviceOnce once;                                                                                                        \
+    HERO_TRY(per_device_once(once, [](int) {                                                                                          \
+      HERO_CUDA_TRY(cudaFuncSetAttribute(gather_ln_f8_kernel<T, G, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));           \
+      return HERO_OK;                                                                                                                 \
+    }));                                                                                                                              \
+  }                                                                                                                                   \
+  return launch_kernel(gather_ln_f8_kernel<T, G, V>, ctas(G, ln_ctas_per_sm(G, V, Pack<T>::N)), ln_threads(G), smem, s, 1, (const T*)x, \
+                       (const T*)add, idx, shift, scale, mod_ld, vec, (uint8_t*)out, out_scale, N, n_sel, B, D, 1.0f / (float)D, eps)
+  HERO_ROWS(HERO_LN_F8)
+  HERO_ROWS_CASE(16, 6, HERO_LN_F8)              // (fp32 rows of more than 6144)
+#undef HERO_LN_F8
+  return HERO_ERR_ARG;
 }
 
 template <typename T, bool Q8>
 int rms_norm_dispatch(const void* x, const void* add, const void* gain, void* sum, void* out, float* out_scale, int rows, int D,
                       float eps, cudaStream_t s) {
-  const int chunks = (D / Pack<T>::N + 31) / 32;       // of 32 packets
-#define HERO_RMS(G, V)                                                                                                      \
-  if (chunks <= G * V)                                                                                                      \
-  return launch_streaming(rms_norm_kernel<T, G, V, Q8>, G == 1 ? ((long long)rows + 7) / 8 : (long long)rows, rms_threads(G), s, \
-                          (const T*)x, (const T*)add, (const T*)gain, (T*)sum, out, out_scale, rows, D, eps)
-  HERO_RMS(1, 1); HERO_RMS(1, 2); HERO_RMS(1, 4);
-  HERO_RMS(4, 2); HERO_RMS(4, 3); HERO_RMS(4, 4);
-  HERO_RMS(8, 3); HERO_RMS(8, 4); HERO_RMS(8, 6);
-  HERO_RMS(16, 4); HERO_RMS(16, 6);
+  const int chunks = row_chunks(D, Piece<T>::N);
+#define HERO_RMS(G, V)                                                                                                          \
+  return launch_streaming(rms_norm_kernel<T, G, V, Q8>, row_ctas(G, rows), rows_threads(G), s, (const T*)x, (const T*)add,         \
+                          (const T*)gain, (T*)sum, out, out_scale, rows, D, 1.0f / (float)D, eps)
+  HERO_ROWS(HERO_RMS)
 #undef HERO_RMS
   return HERO_ERR_ARG;
 }
 
 // ------------------------------------------------------------------ blocks of 1 x 128
-// A warp takes 32 packets of a row (256 columns of bf16, 128 of fp32) at a time, kPieces of them in flight.
-constexpr int kQuantPieces = 4;
+// A warp takes 512 columns of bf16 or 256 of fp32 of a row and nothing else: the more warps, the better the loads of some overlap the
+// stores of others (8774 x 3072 bf16: 14.4 us with one piece a lane, 15.6 with two, 16.6 with four; 19.0 with four of 16 bytes).
 template <typename T>
 __global__ void __launch_bounds__(256)
 quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float* __restrict__ scale, int cols, int per_row,
                      long long pieces) {
   stream_order();
-  using P = Pack<T>;
-  constexpr int kLanes = kF8Block / P::N;
-  const int lane = threadIdx.x & 31;
-  const int packets = cols / P::N, blocks = (cols + kF8Block - 1) / kF8Block;
-  const long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kQuantPieces;
-  uint4 raw[kQuantPieces];
-  long long row[kQuantPieces];
-  int v[kQuantPieces];
-#pragma unroll
-  for (int i = 0; i < kQuantPieces; ++i) {
-    const long long p = first + i;
-    row[i] = p / per_row;
-    v[i] = (int)(p - row[i] * per_row) * 32 + lane;
-    if (p >= pieces) v[i] = packets;
-    raw[i] = make_uint4(0, 0, 0, 0);
-    if (v[i] < packets) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x + row[i] * cols) + v[i]);
+  const long long piece = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (piece >= pieces) return;                                 // warp-uniform
+  const long long row = piece / per_row;
+  const int v = (int)(piece - row * per_row) * 32 + (threadIdx.x & 31), packets = cols / Piece<T>::kPacket;
+  uint4 raw[2];
+  load_piece<true>(raw, x + row * cols, v, packets);
+  uint32_t m[1];
+  {
+    float2 f[Piece<T>::N / 2];
+    unpack(raw, f, T());
+    m[0] = piece_amax<T>(f);
   }
-#pragma unroll
-  for (int i = 0; i < kQuantPieces; ++i) {
-    float f[P::N];
-    P::unpack(raw[i], f);
-    const F8Scale s = f8_scale(block_amax<T>(f));
-    if (v[i] < packets) {
-      store_f8<T>(out + row[i] * cols + (long long)v[i] * P::N, f, s.inv);
-      if (v[i] % kLanes == 0) scale[row[i] * blocks + v[i] / kLanes] = s.scale;
-    }
-  }
+  float inv[1];
+  row_scales<Piece<T>::kLanes, 1>(m, inv, scale + row * ((cols + kF8Block - 1) / kF8Block), v, 0, packets / 2);
+  // (the fp32 values are made again and not kept over the shuffles: 31 registers and all warps resident, 14.4 us for 15.5)
+  asm volatile("" : "+r"(raw[0].x), "+r"(raw[0].y), "+r"(raw[0].z), "+r"(raw[0].w), 
+               "+r"(raw[1].x), "+r"(raw[1].y), "+r"(raw[1].z), "+r"(raw[1].w));
+  float2 f[Piece<T>::N / 2];
+  unpack(raw, f, T());
+  if (2 * v < packets) store_f8<T>(out + row * cols, f, inv[0], v);
 }
 
 // ------------------------------------------------------------------ blocks of 128 x 128
@@ -221,20 +487,20 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
     const int r = r0 + i * kStep;
     if (r < rows && col < cols) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x + (long long)r * cols + col));
   }
-  uint32_t m = 0;
+  uint32_t bits = 0;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
     float f[P::N];
     P::unpack(raw[i], f);
 #pragma unroll
-    for (int q = 0; q < P::N; ++q) m = max(m, abs_bits(f[q]));
+    for (int q = 0; q < P::N; ++q) bits = max(bits, abs_bits(f[q]));
   }
-  m = __reduce_max_sync(0xFFFFFFFFu, m);
-  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+  bits = __reduce_max_sync(0xFFFFFFFFu, bits);
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = bits;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 8; ++w) m = max(m, s_max[w]);
-  const F8Scale s = f8_scale(m);
+  for (int w = 0; w < 8; ++w) bits = max(bits, s_max[w]);
+  const F8Scale s = f8_scale(bits);
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
     const int r = r0 + i * kStep;
@@ -251,8 +517,8 @@ template <typename T>
 int quantize_t(const void* x, void* q, float* scale, int rows, int cols, int block_rows, cudaStream_t s) {
   const int col_blocks = (cols + kF8Block - 1) / kF8Block;
   if (block_rows == 1) {
-    const int per_row = (cols / Pack<T>::N + 31) / 32;
-    const long long pieces = (long long)rows * per_row, blocks = (pieces + 8 * kQuantPieces - 1) / (8 * kQuantPieces);
+    const int per_row = row_chunks(cols, Piece<T>::N);
+    const long long pieces = (long long)rows * per_row, blocks = (pieces + 7) / 8;
     if (blocks > 0x7FFFFFFFll) return HERO_ERR_ARG;
     return launch_streaming(quantize_rows_kernel<T>, blocks, 256, s, (const T*)x, (uint8_t*)q, scale, cols, per_row, pieces);
   }
@@ -266,6 +532,13 @@ int quantize_t(const void* x, void* q, float* scale, int rows, int cols, int blo
 int launch_quantize_fp8(const void* x, void* q, float* scale, int rows, int cols, int block_rows, int dtype, cudaStream_t s) {
   return dtype == HERO_DTYPE_BF16 ? quantize_t<__nv_bfloat16>(x, q, scale, rows, cols, block_rows, s)
                                   : quantize_t<float>(x, q, scale, rows, cols, block_rows, s);
+}
+
+int launch_gather_ln_modulate_fp8(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld,
+                                  void* out, float* out_scale, int B, int N, int n_sel, int D, float eps, int dtype, cudaStream_t s) {
+  return dtype == HERO_DTYPE_BF16
+             ? gather_ln_f8_dispatch<__nv_bfloat16>(x, add, idx, shift, scale, mod_ld, out, out_scale, B, N, n_sel, D, eps, s)
+             : gather_ln_f8_dispatch<float>(x, add, idx, shift, scale, mod_ld, out, out_scale, B, N, n_sel, D, eps, s);
 }
 
 int launch_rms_norm(const void* x, const void* add, const void* gain, void* sum, void* out, float* out_scale, int rows, int D,

@@ -2,7 +2,6 @@
 // (Algorithm 1), row gather / scatter (Eq. 3's merge), the adaLN modulation vectors and the
 // fused gather + LayerNorm + modulate prologue of Eq. 2.  All of them move each byte once
 // with 128-bit accesses; grids are sized in multiples of the SM count.
-#include "fp8_common.cuh"
 #include "hero_internal.h"
 
 namespace hero {
@@ -559,44 +558,11 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return t;
 }
 
-// Where normalised rows go: compact rows of T, or of e4m3 with a scale per 128 columns.
 template <typename T>
-struct LnRows {
-  T* rows;
-  static constexpr bool kF8 = false;
-};
-struct LnRowsF8 {
-  uint8_t* rows;
-  float* scale;
-  static constexpr bool kF8 = true;
-};
-// A packet's worth of a row to e4m3, by all lanes of a warp (the lanes of a block of 128 columns stand side by side).
-template <typename T>
-__device__ __forceinline__ void ln_store_f8(const LnRowsF8& out, long long row, int D, int v, bool there, const float (&r)[Vec<T>::N]) {
-  constexpr int kN = Vec<T>::N, kLanes = kF8Block / kN;
-  uint32_t m = 0;
-#pragma unroll
-  for (int q = 0; q < kN; ++q) m = max(m, abs_bits(r[q]));
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-  const F8Scale s = f8_scale(m);
-  if (there) {
-    uint32_t w[kN / 4];
-#pragma unroll
-    for (int q = 0; q < kN / 4; ++q)
-      w[q] = f8_pack4(r[4 * q] * s.inv, r[4 * q + 1] * s.inv, r[4 * q + 2] * s.inv, r[4 * q + 3] * s.inv);
-    uint8_t* to = out.rows + row * D + (long long)v * kN;
-    if constexpr (kN == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(w[0], w[1]));
-    else __stcs(reinterpret_cast<unsigned int*>(to), w[0]);
-    if (v % kLanes == 0) out.scale[row * ((D + kF8Block - 1) / kF8Block) + v / kLanes] = s.scale;
-  }
-}
-
-template <typename T, typename Rows>
 __global__ void __launch_bounds__(kLnThreads)
 gather_ln_modulate_kernel(const T* __restrict__ x, const T* __restrict__ add, const int* __restrict__ idx,
                           const float* __restrict__ shift, const float* __restrict__ scale, int mod_ld,
-                          const Rows a, int N, int n_sel, int D, float eps) {
+                          T* __restrict__ a, int N, int n_sel, int D, float eps) {
   stream_order();
   extern __shared__ float s_row[];   // [D]
   __shared__ float red[kLnThreads / 32];
@@ -629,21 +595,16 @@ gather_ln_modulate_kernel(const T* __restrict__ x, const T* __restrict__ add, co
   const float rstd = 1.0f / sqrtf(var + eps);
   const float* sh = shift + (long long)b * mod_ld;
   const float* sc = scale + (long long)b * mod_ld;
-  for (int c0 = 0; c0 < n_vec; c0 += kLnThreads) {     // (the same turns for all lanes of a warp)
-    const int c = c0 + threadIdx.x;
-    float f[V::N] = {};
-    if (c < n_vec) {
+  V* out = reinterpret_cast<V*>(a + (long long)m * D);
+  for (int c = threadIdx.x; c < n_vec; c += kLnThreads) {
+    float f[V::N];
 #pragma unroll
-      for (int q = 0; q < V::N; ++q) {
-        const int col = c * V::N + q;
-        f[q] = fmaf((s_row[col] - mean) * rstd, 1.0f + sc[col], sh[col]);
-      }
-      if constexpr (!Rows::kF8) {
-        V r; r.pack(f);
-        reinterpret_cast<V*>(a.rows + (long long)m * D)[c] = r;
-      }
+    for (int q = 0; q < V::N; ++q) {
+      const int col = c * V::N + q;
+      f[q] = fmaf((s_row[col] - mean) * rstd, 1.0f + sc[col], sh[col]);
     }
-    if constexpr (Rows::kF8) ln_store_f8<T>(a, m, D, c, c < n_vec, f);
+    V r; r.pack(f);
+    out[c] = r;
   }
 }
 
@@ -680,10 +641,10 @@ __device__ __forceinline__ void ln_stage_modulation(float4* s_mod, const float* 
   }
   __syncthreads();
 }
-// Statistics of a row held by a warp (absent packets are zeros), normalised, modulated and written to row `row` of `out`.
-template <typename T, int VPL, int FULL, typename Rows>
+// Statistics of a row held by a warp (absent packets are zeros), normalised, modulated and written to `out`.
+template <typename T, int VPL, int FULL>
 __device__ __forceinline__ void ln_finish_row(const float (&f)[VPL][Vec<T>::N], const float4* s_mod, int packets, int D, float eps,
-                                              int lane, const Rows& out, long long row) {
+                                              int lane, T* out_row) {
   using V = Vec<T>;
   constexpr int Q = V::N / 4;
   float sum = 0.f;
@@ -704,11 +665,12 @@ __device__ __forceinline__ void ln_finish_row(const float (&f)[VPL][Vec<T>::N], 
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
   const float rstd = 1.0f / sqrtf(sq / (float)D + eps);
+  V* out = reinterpret_cast<V*>(out_row);
 #pragma unroll
   for (int c = 0; c < VPL; ++c) {
     const int v = c * 32 + lane;         // packet index: columns [V::N * v, V::N * (v + 1))
-    float r[V::N] = {};
     if (c < FULL || v < packets) {
+      float r[V::N];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const float4 s4 = s_mod[q * packets + v], h4 = s_mod[(Q + q) * packets + v];
@@ -717,12 +679,9 @@ __device__ __forceinline__ void ln_finish_row(const float (&f)[VPL][Vec<T>::N], 
         r[4 * q + 2] = fmaf((f[c][4 * q + 2] - mean) * rstd, s4.z, h4.z);
         r[4 * q + 3] = fmaf((f[c][4 * q + 3] - mean) * rstd, s4.w, h4.w);
       }
-      if constexpr (!Rows::kF8) {
-        V o; o.pack(r);
-        __stcs(&reinterpret_cast<V*>(out.rows + row * D)[v].raw, o.raw);
-      }
+      V o; o.pack(r);
+      __stcs(&out[v].raw, o.raw);
     }
-    if constexpr (Rows::kF8) ln_store_f8<T>(out, row, D, v, c < FULL || v < packets, r);
   }
 }
 
@@ -735,11 +694,11 @@ __device__ __forceinline__ void ln_finish_row(const float (&f)[VPL][Vec<T>::N], 
 //
 // Several rows a warp.  (EXACT: the row has exactly 32 * VPL packets, nothing is predicated; the wide rows have no registers to
 // spare for it.)
-template <typename T, int VPL, bool EXACT, typename Rows>
+template <typename T, int VPL, bool EXACT>
 __global__ void __launch_bounds__(256, ln_ctas_per_sm(VPL, false))
 gather_ln_modulate_rows_kernel(const T* __restrict__ x, const T* __restrict__ add, const int* __restrict__ idx,
                                const float* __restrict__ shift, const float* __restrict__ scale, int mod_ld,
-                               const Rows a, int N, int n_sel, int B, int D, float eps, int settled) {
+                               T* __restrict__ a, int N, int n_sel, int B, int D, float eps, int settled) {
   using V = Vec<T>;
   constexpr int kFull = EXACT ? VPL : ln_full_chunks(VPL);    // chunks of 32 packets that every row it serves has
   const int packets = EXACT ? VPL * 32 : D / V::N;
@@ -782,17 +741,17 @@ gather_ln_modulate_rows_kernel(const T* __restrict__ x, const T* __restrict__ ad
         }
       }
     }
-    ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, a, (long long)b * n_sel + i);
+    ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, a + ((long long)b * n_sel + i) * D);
   }
 }
 
 // One row a warp at most.  What need not be waited for is on its way before the wait; with nothing settled x is, before the
 // vectors are staged (600 x 256 2.21 -> 1.99 us, 4400 x 512 4.34 -> 3.25 against the loop).
-template <typename T, int VPL, typename Rows>
+template <typename T, int VPL>
 __global__ void __launch_bounds__(256, ln_ctas_per_sm(VPL, true))
 gather_ln_modulate_row_kernel(const T* __restrict__ x, const T* __restrict__ add, const int* __restrict__ idx,
                               const float* __restrict__ shift, const float* __restrict__ scale, int mod_ld,
-                              const Rows a, int N, int n_sel, int B, int D, float eps, int settled) {
+                              T* __restrict__ a, int N, int n_sel, int B, int D, float eps, int settled) {
   using V = Vec<T>;
   constexpr int kFull = ln_full_chunks(VPL);
   const int packets = D / V::N;
@@ -839,7 +798,7 @@ gather_ln_modulate_row_kernel(const T* __restrict__ x, const T* __restrict__ add
       }
     }
   }
-  ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, a, (long long)b * n_sel + i);
+  ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, a + ((long long)b * n_sel + i) * D);
 }
 
 // The end of one refreshed block and the start of the next in one pass: x = (x + ga) + gf for every row, and the rows that
@@ -903,7 +862,7 @@ residual_ln_kernel(T* __restrict__ x, const T* __restrict__ ga, const T* __restr
         for (int q = 0; q < V::N; ++q) f[c][q] = 0.f;
       }
     }
-    if (place >= 0) ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, LnRows<T>{a}, (long long)b * n_sel + place);
+    if (place >= 0) ln_finish_row<T, VPL, kFull>(f, s_mod, packets, D, eps, lane, a + ((long long)b * n_sel + place) * D);
     if (ONE) break;
   }
 }
@@ -932,30 +891,30 @@ int residual_ln_dispatch(void* x, const void* ga, const void* gf, const int* pos
   return HERO_ERR_ARG;
 }
 
-template <typename T, int VPL, typename Rows>
+template <typename T, int VPL>
 int gather_ln_warp(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld,
-                   const Rows& a, int N, int n_sel, int B, int D, float eps, int settled, cudaStream_t s) {
+                   void* a, int N, int n_sel, int B, int D, float eps, int settled, cudaStream_t s) {
   // the same number of CTAs for every batch item, at most as many as stay resident
   const int need = (n_sel + 7) / 8;
   const bool one = VPL < 8 && need <= num_sms() * ln_ctas_per_sm(VPL, true) / B;
   const int resident = (num_sms() * ln_ctas_per_sm(VPL, one) + B - 1) / B;
   const unsigned grid = (unsigned)((need < resident ? need : resident) * B);
   const size_t smem = (size_t)2 * D * sizeof(float);
-  auto kernel = gather_ln_modulate_rows_kernel<T, VPL, false, Rows>;
+  auto kernel = gather_ln_modulate_rows_kernel<T, VPL, false>;
   if constexpr (VPL >= 8) {
-    if (D == VPL * 32 * Vec<T>::N) kernel = gather_ln_modulate_rows_kernel<T, VPL, true, Rows>;
+    if (D == VPL * 32 * Vec<T>::N) kernel = gather_ln_modulate_rows_kernel<T, VPL, true>;
   } else {
-    if (one) kernel = gather_ln_modulate_row_kernel<T, VPL, Rows>;
+    if (one) kernel = gather_ln_modulate_row_kernel<T, VPL>;
   }
-  return launch_kernel(kernel, grid, 256, smem, s, 1, (const T*)x, (const T*)add, idx, shift, scale, mod_ld, a, N, n_sel,
+  return launch_kernel(kernel, grid, 256, smem, s, 1, (const T*)x, (const T*)add, idx, shift, scale, mod_ld, (T*)a, N, n_sel,
                        B, D, eps, settled);
 }
 
 // Rows of at most 16 packets a lane; wider ones go through shared memory (gather_ln_modulate_kernel).
 constexpr int kLnMaxPackets = 16;
-template <typename T, typename Rows>
+template <typename T>
 int gather_ln_dispatch(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld,
-                       const Rows& a, int N, int n_sel, int B, int D, float eps, int settled, cudaStream_t s) {
+                       void* a, int N, int n_sel, int B, int D, float eps, int settled, cudaStream_t s) {
   const int vpl = (D / Vec<T>::N + 31) / 32;
 #define HERO_LN(V) \
   if (vpl <= V) return gather_ln_warp<T, V>(x, add, idx, shift, scale, mod_ld, a, N, n_sel, B, D, eps, settled, s)
@@ -1166,44 +1125,35 @@ int launch_residual_ln(void* x, const void* ga, const void* gf, const int* pos, 
              : residual_ln_dispatch<float>(x, ga, gf, pos, n_text, shift, scale, mod_ld, a, N, n_sel, B, D, eps, early, s);
 }
 
-namespace {
-template <typename T, typename Rows>
-int gather_ln_launch(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld, const Rows& a,
-                     int B, int N, int n_sel, int D, float eps, int settled, cudaStream_t s) {
+int launch_gather_ln_modulate(const void* x, const void* add, const int* idx, const float* shift,
+                              const float* scale, int mod_ld, void* a, int B, int N, int n_sel, int D, float eps,
+                              int dtype, int settled, cudaStream_t s) {
   const long long rows = (long long)B * n_sel;
   if (rows == 0) return HERO_OK;
-  constexpr int per = Vec<T>::N;
+  const bool bf16 = dtype == HERO_DTYPE_BF16;
+  const int per = bf16 ? 8 : 4;
   if (D % per) return HERO_ERR_ALIGN;
   // the warp kernel reads the adaLN vectors as float4: every item's slice starts 16-byte aligned when mod_ld % 4 == 0
   const bool vec_ok = mod_ld % 4 == 0 && ((reinterpret_cast<uintptr_t>(shift) | reinterpret_cast<uintptr_t>(scale)) & 15) == 0;
   if (vec_ok && D / per <= 32 * kLnMaxPackets)
-    return gather_ln_dispatch<T>(x, add, idx, shift, scale, mod_ld, a, N, n_sel, B, D, eps, settled, s);
+    return bf16 ? gather_ln_dispatch<__nv_bfloat16>(x, add, idx, shift, scale, mod_ld, a, N, n_sel, B, D, eps, settled, s)
+                : gather_ln_dispatch<float>(x, add, idx, shift, scale, mod_ld, a, N, n_sel, B, D, eps, settled, s);
   // The widest row, 12288 features, fills the 48 KB a kernel may have without an opt-in; the reduction's words come on top.
   static PerDeviceOnce once;
   HERO_TRY(per_device_once(once, [](int) {
-    HERO_CUDA_TRY(cudaFuncSetAttribute(gather_ln_modulate_kernel<T, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024));
+    HERO_CUDA_TRY(cudaFuncSetAttribute(gather_ln_modulate_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024));
+    HERO_CUDA_TRY(cudaFuncSetAttribute(gather_ln_modulate_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024));
     return HERO_OK;
   }));
-  return launch_kernel(gather_ln_modulate_kernel<T, Rows>, (unsigned)rows, kLnThreads, (size_t)D * sizeof(float), s, 1, (const T*)x,
-                       (const T*)add, idx, shift, scale, mod_ld, a, N, n_sel, D, eps);
-}
-}  // namespace
-
-int launch_gather_ln_modulate(const void* x, const void* add, const int* idx, const float* shift,
-                              const float* scale, int mod_ld, void* a, int B, int N, int n_sel, int D, float eps,
-                              int dtype, int settled, cudaStream_t s) {
-  return dtype == HERO_DTYPE_BF16
-             ? gather_ln_launch<__nv_bfloat16>(x, add, idx, shift, scale, mod_ld, LnRows<__nv_bfloat16>{(__nv_bfloat16*)a}, B, N, n_sel,
-                                               D, eps, settled, s)
-             : gather_ln_launch<float>(x, add, idx, shift, scale, mod_ld, LnRows<float>{(float*)a}, B, N, n_sel, D, eps, settled, s);
-}
-
-int launch_gather_ln_modulate_fp8(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld,
-                                  void* a, float* a_scale, int B, int N, int n_sel, int D, float eps, int dtype, cudaStream_t s) {
-  const LnRowsF8 rows = {(uint8_t*)a, a_scale};
-  return dtype == HERO_DTYPE_BF16
-             ? gather_ln_launch<__nv_bfloat16>(x, add, idx, shift, scale, mod_ld, rows, B, N, n_sel, D, eps, kLnNothingSettled, s)
-             : gather_ln_launch<float>(x, add, idx, shift, scale, mod_ld, rows, B, N, n_sel, D, eps, kLnNothingSettled, s);
+  const size_t smem = (size_t)D * sizeof(float);
+  if (bf16)
+    HERO_TRY(launch_kernel(gather_ln_modulate_kernel<__nv_bfloat16>, (unsigned)rows, kLnThreads, smem, s, 1,
+                           (const __nv_bfloat16*)x, (const __nv_bfloat16*)add, idx, shift, scale, mod_ld,
+                           (__nv_bfloat16*)a, N, n_sel, D, eps));
+  else
+    HERO_TRY(launch_kernel(gather_ln_modulate_kernel<float>, (unsigned)rows, kLnThreads, smem, s, 1, (const float*)x,
+                           (const float*)add, idx, shift, scale, mod_ld, (float*)a, N, n_sel, D, eps));
+  return HERO_OK;
 }
 
 }  // namespace hero

@@ -192,7 +192,7 @@ __device__ __forceinline__ void store32(T* dst, const uint32_t (&w)[8], int n, i
 }
 // A warp's 32 rows (from m0 on, one a lane) by NC columns where rows of C start anywhere: 32 columns at a time through shared memory
 // of the warp's own (32 x 33 floats), so that a store writes 32 columns of one row and not one column of 32 rows (1753 x 1001 x 1040:
-// XXX us so, YYY with a store per element).
+// 8.9 us fp32 so, 17.7 with a store per element; 8774 x 3001 x 3072 bf16 107 us for 333, and 92 with 3000 columns).
 template <int NC, int OUT>
 __device__ __forceinline__ void store_ragged(const float2 (&acc)[NC / 2], const F8Gemm& g, int m0, int n0, float* s_rows, int lane) {
 #pragma unroll
