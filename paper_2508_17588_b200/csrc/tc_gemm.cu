@@ -59,14 +59,15 @@ int make_tmap_bf16(CUtensorMap* m, const void* base, int rank, const uint64_t* d
   return HERO_OK;
 }
 
-// A byte matrix [rows, cols], rows contiguous; box = box_rows x 128 bytes, swizzle and fill as above.
-int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+// A byte matrix [rows, cols], rows contiguous; box = box_rows x 128 bytes, swizzle and fill as above, or (narrow) box_rows x 64
+// bytes with the 64-byte swizzle.
+int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, bool narrow) {
   HERO_TRY(tc_init_driver_api());
   const cuuint64_t gdim[2] = {cols, rows}, gstr[1] = {cols};
-  const cuuint32_t bx[2] = {128, box_rows}, es[2] = {1, 1};
+  const cuuint32_t bx[2] = {narrow ? 64u : 128u, box_rows}, es[2] = {1, 1};
   CUresult r = g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstr, bx, es,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     return HERO_ERR_CUDA;

@@ -20,7 +20,7 @@
 
 namespace hero {
 
-int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+int make_tmap_bytes(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, bool narrow);
 
 namespace {
 using namespace tc;
@@ -43,14 +43,34 @@ struct F8Gemm {
   int vec;                       // rows of C start on multiples of: 32, 16 or 0 (less) bytes
 };
 
-// GELU-tanh to fp32 accuracy: t (1 + tanh u) / 2 = t / (1 + exp(-2u)).  (bf16 results take the hardware tanh, which is
-// exact enough for their rounding and one special-function instruction less.)
-__device__ __forceinline__ float gelu_exact_f(float t) {
-  const float u = t * fmaf(0.0356774081f, t * t, 0.7978845608f);
-  return __fdividef(t, 1.0f + __expf(-2.0f * u));
+// GELU-tanh to fp32 accuracy: t (1 + tanh u) / 2 = t / (1 + exp(-2u)), u = sqrt(2 / pi) (t + 0.044715 t^3).  Four values share one
+// reciprocal, that of the product of their denominators, so that a value costs 1.25 special-function instructions; the exponential
+// is cut off at 2^30 to keep that product finite (a value below -5.1 then comes out as t 2^-30 instead of something smaller).
+// (bf16 results take the hardware tanh, which is exact enough for their rounding: one special-function instruction.)
+__device__ __forceinline__ float gelu_denominator(float t) {
+  const float x = t * fmaf(-0.10294324f, t * t, -2.3022082f);        // -2 u log2(e)
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(x, 30.f)));
+  return 1.0f + e;
+}
+__device__ __forceinline__ void gelu_exact4(float2& a, float2& b) {
+  const float d0 = gelu_denominator(a.x), d1 = gelu_denominator(a.y), d2 = gelu_denominator(b.x), d3 = gelu_denominator(b.y);
+  const float d01 = d0 * d1, d23 = d2 * d3;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d01 * d23));
+  const float r01 = r * d23, r23 = r * d01;
+  a = make_float2(a.x * (r01 * d1), a.y * (r01 * d0));
+  b = make_float2(b.x * (r23 * d3), b.y * (r23 * d2));
 }
 template <int OUT>
-__device__ __forceinline__ float gelu(float t) { return OUT == kOutBf16 ? gelu_tanh_f(t) : gelu_exact_f(t); }
+__device__ __forceinline__ void gelu4(float2& a, float2& b) {
+  if constexpr (OUT == kOutBf16) {
+    a = make_float2(gelu_tanh_f(a.x), gelu_tanh_f(a.y));
+    b = make_float2(gelu_tanh_f(b.x), gelu_tanh_f(b.y));
+  } else {
+    gelu_exact4(a, b);
+  }
+}
 
 // Wait for columns asked for with tmem_ld.  The registers are named behind it, two at a time, so that nothing that uses them moves
 // ahead of the wait.
@@ -165,7 +185,7 @@ __device__ __forceinline__ void finish_row(float2 (&acc)[NC / 2], const float* s
   }
   if (act) {
 #pragma unroll
-    for (int i = 0; i < NC / 2; ++i) acc[i] = make_float2(gelu<OUT>(acc[i].x), gelu<OUT>(acc[i].y));
+    for (int i = 0; i < NC / 2; i += 2) gelu4<OUT>(acc[i], acc[i + 1]);
   }
 }
 template <int NC>
@@ -217,37 +237,63 @@ __device__ __forceinline__ void store_ragged(const float2 (&acc)[NC / 2], const 
     }
   }
 }
+// 32 bytes of results: columns [v * kPer, (v + 1) * kPer) of a row's NC.
+template <int OUT>
+constexpr int kPer32 = OUT == kOutF32 ? 8 : (OUT == kOutBf16 ? 16 : 32);
+template <int NC, int OUT>
+__device__ __forceinline__ void pack32(uint32_t (&w)[8], const float2 (&acc)[NC / 2], int v, float inv) {
+  const float2* a = &acc[v * (kPer32<OUT> / 2)];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (OUT == kOutF32) w[i] = __float_as_uint(i & 1 ? a[i / 2].y : a[i / 2].x);
+    else if constexpr (OUT == kOutBf16) w[i] = bf16x2(a[i]);
+    else w[i] = f8_pack4(a[2 * i].x * inv, a[2 * i].y * inv, a[2 * i + 1].x * inv, a[2 * i + 1].y * inv);
+  }
+}
+template <int OUT>
+struct OutType { typedef float T; };
+template <>
+struct OutType<kOutBf16> { typedef __nv_bfloat16 T; };
+template <>
+struct OutType<kOutF8> { typedef uint8_t T; };
 template <int NC, int OUT>
 __device__ __forceinline__ void store_row(const float2 (&acc)[NC / 2], const F8Gemm& g, int m, int n0, float inv) {
-  if constexpr (OUT == kOutF32) {
-    float* dst = static_cast<float*>(g.c) + (long long)m * g.N + n0;
+  typename OutType<OUT>::T* dst = static_cast<typename OutType<OUT>::T*>(g.c) + (long long)m * g.N + n0;
 #pragma unroll
-    for (int v = 0; v < NC / 8; ++v) {
+  for (int v = 0; v < NC / kPer32<OUT>; ++v) {
+    uint32_t w[8];
+    pack32<NC, OUT>(w, acc, v, inv);
+    store32(dst + v * kPer32<OUT>, w, n0 + v * kPer32<OUT>, g.N, g.vec);
+  }
+}
+// A warp's 32 rows (from m0 on, one a lane) by NC columns, 64 bytes of each at a time through two buffers of shared memory (2 KB each, the
+// 64-byte swizzle of the tensor map) and TMA.  A lane's own 32-byte stores touch 32 lines an instruction: 8774 x 12288 x 3072 with bf16
+// results XXX us so, 408 with them.
+template <int NC, int OUT>
+__device__ __forceinline__ void store_tma(const float2 (&acc)[NC / 2], const F8Gemm& g, const CUtensorMap* tm_c, int m0, int n0, float inv,
+                                          uint32_t s_rows, int lane) {
+  constexpr int kCols = 2 * kPer32<OUT>, kSize = (int)sizeof(typename OutType<OUT>::T);
+#pragma unroll
+  for (int q = 0; q < NC / kCols; ++q) {
+    const uint32_t buf = s_rows + (q & 1) * 2048, to = buf + lane * 64, turn = (lane >> 1) & 3;
+    if (lane == 0) tma_store_wait_read<1>();
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
       uint32_t w[8];
+      pack32<NC, OUT>(w, acc, 2 * q + h, inv);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { w[2 * i] = __float_as_uint(acc[4 * v + i].x); w[2 * i + 1] = __float_as_uint(acc[4 * v + i].y); }
-      store32(dst + v * 8, w, n0 + v * 8, g.N, g.vec);
+      for (int k = 0; k < 2; ++k)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * h + k) ^ turn) << 4)), "r"(w[4 * k]), "r"(w[4 * k + 1]),
+                     "r"(w[4 * k + 2]), "r"(w[4 * k + 3])
+                     : "memory");
     }
-  } else if constexpr (OUT == kOutBf16) {
-    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(g.c) + (long long)m * g.N + n0;
-#pragma unroll
-    for (int v = 0; v < NC / 16; ++v) {
-      uint32_t w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = bf16x2(acc[8 * v + i]);
-      store32(dst + v * 16, w, n0 + v * 16, g.N, g.vec);
-    }
-  } else {
-    uint8_t* dst = static_cast<uint8_t*>(g.c) + (long long)m * g.N + n0;
-#pragma unroll
-    for (int v = 0; v < NC / 32; ++v) {
-      uint32_t w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 a = acc[16 * v + 2 * i], b = acc[16 * v + 2 * i + 1];
-        w[i] = f8_pack4(a.x * inv, a.y * inv, b.x * inv, b.y * inv);
-      }
-      store32(dst + v * 32, w, n0 + v * 32, g.N, g.vec);
+    proxy_fence_shared();
+    __syncwarp();
+    if (lane == 0) {
+      const int n = n0 + q * kCols;
+      if (m0 < g.M && n < g.N) tma_store_2d(tm_c, buf, n * kSize, m0);
+      tma_store_commit();
     }
   }
 }
@@ -259,22 +305,20 @@ __device__ __forceinline__ float put_scale(const F8Gemm& g, uint32_t amax, int m
 }
 // Finish and store NC columns of a warp's 32 rows, m this lane's; s_rows: see store_ragged.  e4m3: the two warps that hold the halves
 // of a block trade their maxima through `s_amax` (two words a row) and `meet`, a barrier of theirs for two arrivals, used once; the
-// wait is bounded like every other (NC = 128 is a block by itself).
+// wait is bounded like every other.
 template <int NC, int OUT>
 __device__ __forceinline__ void emit_rows(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, float* s_rows,
                                           uint32_t* s_amax, uint64_t* meet, int which, volatile int* abort_flag) {
   const int lane = threadIdx.x & 31;
   finish_row<NC, OUT>(acc, s_bias, g.act);
   if constexpr (OUT == kOutF8) {
+    static_assert(2 * NC == kF8Block, "two warps hold a block");
     uint32_t amax = row_amax<NC>(acc);
-    if constexpr (NC < kF8Block) {
-      static_assert(2 * NC == kF8Block || OUT != kOutF8, "two warps hold a block");
-      s_amax[which * 32 + lane] = amax;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(meet);
-      if (!mbar_wait_warp(meet, 0, abort_flag)) return;
-      amax = max(amax, s_amax[(which ^ 1) * 32 + lane]);
-    }
+    s_amax[which * 32 + lane] = amax;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(meet);
+    if (!mbar_wait_warp(meet, 0, abort_flag)) return;
+    amax = max(amax, s_amax[(which ^ 1) * 32 + lane]);
     const float inv = put_scale(g, amax, m, n0, which == 0);
     if (m < g.M) store_row<NC, OUT>(acc, g, m, n0, inv);
   } else if (g.vec) {
@@ -282,6 +326,16 @@ __device__ __forceinline__ void emit_rows(float2 (&acc)[NC / 2], const F8Gemm& g
   } else {
     store_ragged<NC, OUT>(acc, g, m - lane, n0, s_rows, lane);
   }
+}
+// The same for a whole block of columns a thread, through TMA where the rows allow it.
+template <int OUT>
+__device__ __forceinline__ void emit_block(float2 (&acc)[kF8Block / 2], const F8Gemm& g, const CUtensorMap* tm_c, const float* s_bias, int m,
+                                           int n0, float* s_rows, int lane) {
+  finish_row<kF8Block, OUT>(acc, s_bias, g.act);
+  float inv = 0.f;
+  if constexpr (OUT == kOutF8) inv = put_scale(g, row_amax<kF8Block>(acc), m, n0, true);
+  if (OUT == kOutF8 || g.vec) store_tma<kF8Block, OUT>(acc, g, tm_c, m - lane, n0, inv, smem_u32(s_rows), lane);
+  else if constexpr (OUT != kOutF8) store_ragged<kF8Block, OUT>(acc, g, m - lane, n0, s_rows, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -504,10 +558,10 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       const int n = n0 + tile_row;
       const float b = g.bias != nullptr && n < g.N ? __bfloat162float(__ldg(g.bias + n)) : 0.f;
 #pragma unroll
-      for (int c = 0; c < BN; ++c) {
-        float& v = c & 1 ? acc[c / 2].y : acc[c / 2].x;
-        v += b;
-        if (g.act) v = gelu<OUT>(v);
+      for (int i = 0; i < BN / 2; ++i) acc[i] = __fadd2_rn(acc[i], make_float2(b, b));
+      if (g.act) {
+#pragma unroll
+        for (int i = 0; i < BN / 2; i += 2) gelu4<OUT>(acc[i], acc[i + 1]);
       }
       F8Scale sc = {};
       if constexpr (OUT == kOutF8) {         // the 128 rows of W are a block: a column's maximum over the four warps
@@ -571,7 +625,8 @@ struct PairCfg {
 
 template <int OUT>
 __global__ void __launch_bounds__(PairCfg::kThreads, 1)
-fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const F8Gemm g,
+fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
+                const __grid_constant__ CUtensorMap tm_c, const F8Gemm g,
                 int* __restrict__ status) {
   using Cfg = PairCfg;
   constexpr int kStages = Cfg::kStages, kCols = Cfg::kCols, BN = Cfg::kBN, kPromote = Cfg::kPromote, kWindow = ScaleBlock::kBlocks;
@@ -579,10 +634,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
   // The dynamic shared memory starts at the same offset in both CTAs, and so does everything carved from it: a
   // descriptor or a barrier offset means the same place in either.
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  float* s_bias_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);
+  float* s_rows_all = reinterpret_cast<float*>(smem + (size_t)kStages * Cfg::kStageBytes);      // (on a multiple of 1024 bytes)
+  float* s_bias_all = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_rows_all) + Cfg::kRowsBytes);
   float* s_scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_bias_all) + Cfg::kBiasBytes);
-  float* s_rows_all = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_rows_all) + Cfg::kRowsBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_scale) + Cfg::kScaleBytes);
   uint64_t* full = bars;                    // [kStages] both CTAs' TMA -> MMA (the even CTA's is the one in use)
   uint64_t* empty = bars + kStages;         // [kStages] MMA -> TMA (each CTA its own)
   uint64_t* acc_full = bars + 2 * kStages;  // [2] MMA -> promotion (each CTA its own)
@@ -606,7 +661,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     *abort_flag = 0;
     mbar_fence_init();
   }
-  if (warp == 0 && lane == 0) { tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_w); }
+  if (warp == 0 && lane == 0) { tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_w); if (OUT == kOutF8 || g.vec) tma_prefetch_desc(&tm_c); }
   if (warp == 3) tmem_alloc_pair(tmem_slot, Cfg::kTmemCols);
   tc_fence_before();
   __syncwarp();
@@ -688,6 +743,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     const int quad = warp & 3;                 // TMEM lane quadrant this warp may read
     const int half = (warp - 4) >> 2;          // which half of the tile's columns it has
     float* s_bias = s_bias_all + (size_t)(warp - 4) * kCols;
+    // (a warp's rows lie 4224 bytes apart for store_ragged and 4096 for TMA, which wants the alignment)
+    float* s_rows = s_rows_all + (warp - 4) * (OUT == kOutF8 || g.vec ? 1024 : 32 * 33);
     const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
     const uint32_t full_bar = smem_u32(acc_full), empty_bar = cluster_map(smem_u32(acc_empty), 0);
     uint32_t w = 0;                            // windows of scales so far
@@ -768,8 +825,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
       }
       tmem_wait(r[0]);
       ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0);
-      if (ok) emit_rows<kCols, OUT>(acc, g, s_bias, m, n_first, s_rows_all + (warp - 4) * 32 * 33, nullptr, nullptr, 0, abort_flag);
+      if (ok) emit_block<OUT>(acc, g, &tm_c, s_bias, m, n_first, s_rows, lane);
     }
+    if (lane == 0) tma_store_wait_all();       // (nothing is in flight from shared memory when the CTA ends)
   }
 
   // ---------------------------------------------------------------- teardown
@@ -781,7 +839,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
 }
 
 template <int OUT>
-int launch_pair(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
+int launch_pair(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const CUtensorMap& tm_c, const F8Gemm& g, int* d_status, cudaStream_t s) {
   static PerDeviceOnce attr_once;            // the opt-in is a property of the kernel ON a device
   HERO_TRY(per_device_once(attr_once, [](int) {
     HERO_CUDA_TRY(cudaFuncSetAttribute(fp8_pair_kernel<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg::kSmem));
@@ -790,7 +848,7 @@ int launch_pair(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& 
   const long long tiles = (long long)((g.M - 1) / (2 * kRows) + 1) * ((g.N - 1) / PairCfg::kBN + 1);
   if (tiles > 0x3FFFFFFF) return HERO_ERR_ARG;
   const int pairs = tiles < num_sms() / 2 ? (int)tiles : num_sms() / 2;
-  return launch_kernel(fp8_pair_kernel<OUT>, (unsigned)(2 * pairs), PairCfg::kThreads, PairCfg::kSmem, s, 2, tm_a, tm_w, g, d_status);
+  return launch_kernel(fp8_pair_kernel<OUT>, (unsigned)(2 * pairs), PairCfg::kThreads, PairCfg::kSmem, s, 2, tm_a, tm_w, tm_c, g, d_status);
 }
 
 template <int BN, bool SWAP, int OUT>
@@ -810,8 +868,8 @@ int launch_split(const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm&
 }
 
 template <int OUT>
-int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensorMap& tm_w, const F8Gemm& g, int* d_status, cudaStream_t s) {
-  if (plan.split == 0) return launch_pair<OUT>(tm_a, tm_w, g, d_status, s);
+int launch_out(const TcGemmF8Plan& plan, const CUtensorMap& tm_a, const CUtensorMap& tm_w, const CUtensorMap& tm_c, const F8Gemm& g, int* d_status, cudaStream_t s) {
+  if (plan.split == 0) return launch_pair<OUT>(tm_a, tm_w, tm_c, g, d_status, s);
   if (plan.swap) return launch_split<16, true, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
   if constexpr (OUT != kOutF8)
     if (plan.bn == 64) return launch_split<64, false, OUT>(tm_a, tm_w, g, plan.split, d_status, s);
@@ -871,17 +929,18 @@ TcGemmF8Plan plan_tc_gemm_fp8(int M, int Nout, int K, bool f8_out, int sms) {
 int launch_tc_gemm_fp8(const void* a, const float* a_scale, const void* w, const float* w_scale, const void* bias, void* c,
                        float* c_scale, int M, int Nout, int K, int act, int out_dtype, int* d_status, cudaStream_t s) {
   const TcGemmF8Plan plan = plan_tc_gemm_fp8(M, Nout, K, out_dtype == HERO_DTYPE_E4M3, num_sms());
-  CUtensorMap tm_a, tm_w;
-  HERO_TRY(make_tmap_bytes(&tm_a, a, (uint64_t)M, (uint64_t)K, plan.swap ? plan.bn : kRows));
-  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? PairCfg::kCols : (plan.swap ? kRows : plan.bn)));
   F8Gemm g = {a_scale, w_scale, static_cast<const __nv_bfloat16*>(bias), c, c_scale, M, Nout, K, act, 0};
-  const unsigned long long low = (unsigned long long)reinterpret_cast<uintptr_t>(c) |
-                                 (unsigned long long)Nout * (out_dtype == HERO_DTYPE_FP32 ? 4 : (out_dtype == HERO_DTYPE_BF16 ? 2 : 1));
+  const int size = out_dtype == HERO_DTYPE_FP32 ? 4 : (out_dtype == HERO_DTYPE_BF16 ? 2 : 1);
+  const unsigned long long low = (unsigned long long)reinterpret_cast<uintptr_t>(c) | (unsigned long long)Nout * size;
   g.vec = low % 32 == 0 ? 32 : (low % 16 == 0 ? 16 : 0);
+  CUtensorMap tm_a, tm_w, tm_c = {};
+  HERO_TRY(make_tmap_bytes(&tm_a, a, (uint64_t)M, (uint64_t)K, plan.swap ? plan.bn : kRows, false));
+  HERO_TRY(make_tmap_bytes(&tm_w, w, (uint64_t)Nout, (uint64_t)K, plan.split == 0 ? PairCfg::kCols : (plan.swap ? kRows : plan.bn), false));
+  if (plan.split == 0 && g.vec) HERO_TRY(make_tmap_bytes(&tm_c, c, (uint64_t)M, (uint64_t)Nout * size, 32, true));
   switch (out_dtype) {
-    case HERO_DTYPE_FP32: return launch_out<kOutF32>(plan, tm_a, tm_w, g, d_status, s);
-    case HERO_DTYPE_BF16: return launch_out<kOutBf16>(plan, tm_a, tm_w, g, d_status, s);
-    default: return launch_out<kOutF8>(plan, tm_a, tm_w, g, d_status, s);
+    case HERO_DTYPE_FP32: return launch_out<kOutF32>(plan, tm_a, tm_w, tm_c, g, d_status, s);
+    case HERO_DTYPE_BF16: return launch_out<kOutBf16>(plan, tm_a, tm_w, tm_c, g, d_status, s);
+    default: return launch_out<kOutF8>(plan, tm_a, tm_w, tm_c, g, d_status, s);
   }
 }
 
