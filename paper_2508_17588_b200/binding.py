@@ -410,7 +410,7 @@ def _f8_call(name: str, device: int, tensors: tuple, args: tuple) -> None:
                                      f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
         ptrs.append(t.data_ptr())
     call = getattr(load(), name)
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         code = call(*ptrs, *args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):

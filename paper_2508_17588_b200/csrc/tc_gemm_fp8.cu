@@ -45,13 +45,20 @@ struct F8Gemm {
 
 // GELU-tanh to fp32 accuracy: t (1 + tanh u) / 2 = t / (1 + exp(-2u)), u = sqrt(2 / pi) (t + 0.044715 t^3).  Four values share one
 // reciprocal, that of the product of their denominators, so that a value costs 1.25 special-function instructions; the exponential
-// is cut off at 2^30 to keep that product finite (a value below -5.1 then comes out as t 2^-30 instead of something smaller).
-// (bf16 results take the hardware tanh, which is exact enough for their rounding: one special-function instruction.)
+// is cut off at 2^30 to keep that product finite and t at -16 where it multiplies: a value below -5.1 comes out as something between
+// zero and -16 * 2^-30, less than what fp32 makes of 1 + tanh u there.
+// (bf16 results take the hardware tanh, which is exact enough for their rounding: one special-function instruction.  Scalar
+// arithmetic: packed, the constants take registers that the 128 sums need, and 8774 x 12288 x 3072 454 us for 417.)
 __device__ __forceinline__ float gelu_denominator(float t) {
   const float x = t * fmaf(-0.10294324f, t * t, -2.3022082f);        // -2 u log2(e)
   float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(x, 30.f)));
   return 1.0f + e;
+}
+__device__ __forceinline__ float gelu_factor(float t) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(t), "f"(-16.f));
+  return r;
 }
 __device__ __forceinline__ void gelu_exact4(float2& a, float2& b) {
   const float d0 = gelu_denominator(a.x), d1 = gelu_denominator(a.y), d2 = gelu_denominator(b.x), d3 = gelu_denominator(b.y);
@@ -59,8 +66,8 @@ __device__ __forceinline__ void gelu_exact4(float2& a, float2& b) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d01 * d23));
   const float r01 = r * d23, r23 = r * d01;
-  a = make_float2(a.x * (r01 * d1), a.y * (r01 * d0));
-  b = make_float2(b.x * (r23 * d3), b.y * (r23 * d2));
+  a = make_float2(gelu_factor(a.x) * (r01 * d1), gelu_factor(a.y) * (r01 * d0));
+  b = make_float2(gelu_factor(b.x) * (r23 * d3), gelu_factor(b.y) * (r23 * d2));
 }
 template <int OUT>
 __device__ __forceinline__ void gelu4(float2& a, float2& b) {
@@ -268,7 +275,7 @@ __device__ __forceinline__ void store_row(const float2 (&acc)[NC / 2], const F8G
 }
 // A warp's 32 rows (from m0 on, one a lane) by NC columns, 64 bytes of each at a time through two buffers of shared memory (2 KB each, the
 // 64-byte swizzle of the tensor map) and TMA.  A lane's own 32-byte stores touch 32 lines an instruction: 8774 x 12288 x 3072 with bf16
-// results XXX us so, 408 with them.
+// results 381 us so, 421 with them.
 template <int NC, int OUT>
 __device__ __forceinline__ void store_tma(const float2 (&acc)[NC / 2], const F8Gemm& g, const CUtensorMap* tm_c, int m0, int n0, float inv,
                                           uint32_t s_rows, int lane) {

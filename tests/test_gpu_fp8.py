@@ -269,6 +269,23 @@ def test_gemm_what_is_not_finite_stays_in_its_row(M):
             assert torch.isnan(s2[1:3]).all() and torch.isfinite(s2[3:]).all()
 
 
+@pytest.mark.parametrize("out", ["bf16", "fp32", "e4m3"])
+@pytest.mark.parametrize("M", [3, 70, 2600])
+def test_gemm_gelu_of_large_magnitudes(M, out):
+    """Far below zero GELU is zero and far above it the identity, whatever the magnitude: sums of 1e2, 1e10 and 1e20, one sign a row."""
+    N, K = 2608 if M > 2000 else 272, 144
+    a = np.ones((M, K), np.float32)
+    a_s = np.repeat(np.array([[1e0], [-1e0], [-1e8], [1e8], [-1e18], [1e18]], np.float32), 2, 1)[np.arange(M) % 6]
+    w, w_s = np.ones((N, K), np.float32), np.ones((R.blocks(N), 2), np.float32)
+    c, c_scale = new((M, N), out), new((M, R.blocks(N)), "fp32") if out == "e4m3" else None
+    up = lambda t: torch.from_numpy(np.ascontiguousarray(t)).cuda()  # noqa: E731
+    H().hero_gemm_fp8(up(a).to(F8), up(a_s), up(w).to(F8), up(w_s), None, c, c_scale, act=1)
+    got = host32(c).astype(np.float64) if out != "e4m3" else R.dequantize(host32(c), host32(c_scale), 1)
+    want = np.maximum(a_s[:, :1].astype(np.float64) * K, 0.0)
+    # sums of equal terms, exact but for the scales' product; 16 * 2^-30 is what a value far below zero may leave; half a step of the type
+    assert (np.abs(got - want) <= 2.0 ** -25 + (R.HALF[out] + 2.0 ** -22) * want).all()
+
+
 def test_gemm_leaves_what_is_behind_its_result_alone():
     for M, N, out in ((3, 130, "bf16"), (70, 130, "fp32"), (200, 1001, "bf16"), (200, 272, "e4m3"), (9, 272, "e4m3")):
         _, dev = operands(np.random.default_rng(3), M, N, 272, True)
