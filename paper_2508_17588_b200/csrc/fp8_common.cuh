@@ -19,6 +19,14 @@ constexpr float kF8ScaleFloor = 1.17549435e-38f; // 2^-126
 // maximum carries both through.
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// The largest of m and the magnitudes of a and b, NaN if one of them is NaN (whose bits are then above infinity's): one
+// instruction for two values where the integer maximum takes four (35552 x 3072 bf16 to e4m3 50.9 us for 52.2).
+__device__ __forceinline__ float max_abs3(float m, float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+  return r;
+}
+
 struct F8Scale { float scale, inv; };
 __device__ __forceinline__ F8Scale f8_scale(uint32_t amax_bits) {
   F8Scale r;

@@ -75,6 +75,9 @@ __device__ __forceinline__ void row_scales(uint32_t (&m)[V], float (&inv)[V], fl
   for (int c = 0; c < V; ++c) inv[c] = V == 1 ? s.inv : __shfl_sync(0xFFFFFFFFu, s.inv, (lane & ~(LANES - 1)) | c);
 }
 
+// What was made of `r` so far is made again where it is needed next and not kept in registers meanwhile.
+__device__ __forceinline__ void again(uint4& r) { asm volatile("" : "+r"(r.x), "+r"(r.y), "+r"(r.z), "+r"(r.w)); }
+
 // ------------------------------------------------------------------ 32 bytes of a lane
 // A lane's piece of a row: two packets of 16 bytes, N elements as pairs; kLanes of them are a block of 128 columns.
 template <typename T>
@@ -121,10 +124,10 @@ __device__ __forceinline__ void store_piece(void* row, const uint4 (&r)[2], int 
 }
 template <typename T>
 __device__ __forceinline__ uint32_t piece_amax(const float2 (&f)[Piece<T>::N / 2]) {
-  uint32_t m = 0;
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < Piece<T>::N / 2; ++i) m = max(max(m, abs_bits(f[i].x)), abs_bits(f[i].y));
-  return m;
+  for (int i = 0; i < Piece<T>::N / 2; ++i) m = max_abs3(m, f[i].x, f[i].y);
+  return __float_as_uint(m);
 }
 // Piece v of a row to e4m3 (`row`: the row's bytes).
 template <typename T>
@@ -333,47 +336,50 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
     }
   }
   for (long long i = first; i < n_sel; i += step) {            // (the same turns for a row's threads)
-    float2 f[V][N / 2];
-    float2 sum = make_float2(0.f, 0.f), sq = make_float2(0.f, 0.f);
+    float f[V][N];
+    float sum[2] = {0.f, 0.f}, sq[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      P::unpack(vx[c], reinterpret_cast<float(&)[N]>(f[c]));
+      P::unpack(vx[c], f[c]);
       if (add) {
-        float2 a[N / 2];
-        P::unpack(va[c], reinterpret_cast<float(&)[N]>(a));
+        float a[N];
+        P::unpack(va[c], a);
 #pragma unroll
-        for (int q = 0; q < N / 2; ++q) f[c][q] = __fadd2_rn(f[c][q], a[q]);
+        for (int q = 0; q < N; ++q) f[c][q] += a[q];
       }
 #pragma unroll
-      for (int q = 0; q < N / 2; ++q) sum = __fadd2_rn(sum, f[c][q]);
+      for (int q = 0; q < N; ++q) sum[q & 1] += f[c][q];
     }
     fetch(i + step);
     look(i + 2 * step);
-    const float mean = total(sum, s_part[0]) * inv_d;
+    const float mean = total(make_float2(sum[0], sum[1]), s_part[0]) * inv_d;
 #pragma unroll
     for (int c = 0; c < V; ++c)
       if (c * 32 * G + t < packets) {            // (absent packets stay zeros)
 #pragma unroll
-        for (int q = 0; q < N / 2; ++q) {
-          f[c][q] = __fadd2_rn(f[c][q], make_float2(-mean, -mean));
-          sq = __ffma2_rn(f[c][q], f[c][q], sq);
+        for (int q = 0; q < N; ++q) {
+          f[c][q] -= mean;
+          sq[q & 1] = fmaf(f[c][q], f[c][q], sq[q & 1]);
         }
       }
-    const float rstd = rsqrtf(fmaf(total(sq, s_part[1]), inv_d, eps));
+    const float rstd = rsqrtf(fmaf(total(make_float2(sq[0], sq[1]), s_part[1]), inv_d, eps));
     uint32_t m[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      m[c] = 0;
+      float most = 0.f;
       if (c * 32 * G + t < packets) {
 #pragma unroll
         for (int q = 0; q < N / 4; ++q) {
           const float4 s4 = s_mod[((c * 2) * (N / 4) + q) * kThreads + threadIdx.x], h4 = s_mod[((c * 2 + 1) * (N / 4) + q) * kThreads + threadIdx.x];
-          float2 &u = f[c][2 * q], &w = f[c][2 * q + 1];
-          u = __ffma2_rn(__fmul2_rn(u, make_float2(rstd, rstd)), make_float2(s4.x, s4.y), make_float2(h4.x, h4.y));
-          w = __ffma2_rn(__fmul2_rn(w, make_float2(rstd, rstd)), make_float2(s4.z, s4.w), make_float2(h4.z, h4.w));
-          m[c] = max(max(m[c], max(abs_bits(u.x), abs_bits(u.y))), max(abs_bits(w.x), abs_bits(w.y)));
+          float* u = &f[c][4 * q];
+          u[0] = fmaf(u[0] * rstd, s4.x, h4.x);
+          u[1] = fmaf(u[1] * rstd, s4.y, h4.y);
+          u[2] = fmaf(u[2] * rstd, s4.z, h4.z);
+          u[3] = fmaf(u[3] * rstd, s4.w, h4.w);
+          most = max_abs3(max_abs3(most, u[0], u[1]), u[2], u[3]);
         }
       }
+      m[c] = __float_as_uint(most);
     }
     const long long row = (long long)b * n_sel + i;
     float inv[V];
@@ -381,7 +387,7 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       const int v = c * 32 * G + t;
-      if (v < packets) store_f8<T>(out + row * D + (long long)v * N, reinterpret_cast<const float(&)[N]>(f[c]), inv[c]);
+      if (v < packets) store_f8<T>(out + row * D + (long long)v * N, f[c], inv[c]);
     }
   }
 }
@@ -459,9 +465,8 @@ quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float* 
   }
   float inv[1];
   row_scales<Piece<T>::kLanes, 1>(m, inv, scale + row * ((cols + kF8Block - 1) / kF8Block), v, 0, packets / 2);
-  // (the fp32 values are made again and not kept over the shuffles: 31 registers and all warps resident, 14.4 us for 15.5)
-  asm volatile("" : "+r"(raw[0].x), "+r"(raw[0].y), "+r"(raw[0].z), "+r"(raw[0].w), 
-               "+r"(raw[1].x), "+r"(raw[1].y), "+r"(raw[1].z), "+r"(raw[1].w));
+  again(raw[0]);               // (31 registers and all warps resident: 14.4 us for 15.5)
+  again(raw[1]);
   float2 f[Piece<T>::N / 2];
   unpack(raw, f, T());
   if (2 * v < packets) store_f8<T>(out + row * cols, f, inv[0], v);
@@ -487,15 +492,15 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
     const int r = r0 + i * kStep;
     if (r < rows && col < cols) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x + (long long)r * cols + col));
   }
-  uint32_t bits = 0;
+  float m[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
     float f[P::N];
     P::unpack(raw[i], f);
 #pragma unroll
-    for (int q = 0; q < P::N; ++q) bits = max(bits, abs_bits(f[q]));
+    for (int q = 0; q < P::N; q += 2) m[i & 1] = max_abs3(m[i & 1], f[q], f[q + 1]);
   }
-  bits = __reduce_max_sync(0xFFFFFFFFu, bits);
+  uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(max_abs3(0.f, m[0], m[1])));
   if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = bits;
   __syncthreads();
 #pragma unroll
@@ -506,6 +511,7 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
     const int r = r0 + i * kStep;
     if (r < rows && col < cols) {
       float f[P::N];
+      again(raw[i]);           // (12288 x 3072 bf16: 19.4 us, and 22 with the 64 values kept)
       P::unpack(raw[i], f);
       store_f8<T>(out + (long long)r * cols + col, f, s.inv);
     }

@@ -197,10 +197,10 @@ __device__ __forceinline__ void finish_row(float2 (&acc)[NC / 2], const float* s
 }
 template <int NC>
 __device__ __forceinline__ uint32_t row_amax(const float2 (&acc)[NC / 2]) {
-  uint32_t m = 0;
+  float m[2] = {0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < NC / 2; ++i) m = max(m, max(abs_bits(acc[i].x), abs_bits(acc[i].y)));
-  return m;
+  for (int i = 0; i < NC / 2; ++i) m[i & 1] = max_abs3(m[i & 1], acc[i].x, acc[i].y);
+  return __float_as_uint(max_abs3(0.f, m[0], m[1]));
 }
 __device__ __forceinline__ uint32_t bf16x2(float2 f) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(f.x, f.y);
