@@ -436,7 +436,7 @@ int rms_norm_dispatch(const void* x, const void* add, const void* gain, void* su
                       float eps, cudaStream_t s) {
   const int chunks = row_chunks(D, Piece<T>::N);
 #define HERO_RMS(G, V)                                                                                                          \
-  return launch_streaming(rms_norm_kernel<T, G, V, Q8>, row_ctas(G, rows), rows_threads(G), s, (const T*)x, (const T*)add,         \
+  return launch_kernel(rms_norm_kernel<T, G, V, Q8>, (unsigned)row_ctas(G, rows), rows_threads(G), 0, s, 1, (const T*)x, (const T*)add,         \
                           (const T*)gain, (T*)sum, out, out_scale, rows, D, 1.0f / (float)D, eps)
   HERO_ROWS(HERO_RMS)
 #undef HERO_RMS
@@ -526,11 +526,11 @@ int quantize_t(const void* x, void* q, float* scale, int rows, int cols, int blo
     const int per_row = row_chunks(cols, Piece<T>::N);
     const long long pieces = (long long)rows * per_row, blocks = (pieces + 7) / 8;
     if (blocks > 0x7FFFFFFFll) return HERO_ERR_ARG;
-    return launch_streaming(quantize_rows_kernel<T>, blocks, 256, s, (const T*)x, (uint8_t*)q, scale, cols, per_row, pieces);
+    return launch_kernel(quantize_rows_kernel<T>, (unsigned)blocks, 256, 0, s, 1, (const T*)x, (uint8_t*)q, scale, cols, per_row, pieces);
   }
   const long long blocks = (long long)((rows + (long long)kF8Block - 1) / kF8Block) * col_blocks;
   if (blocks > 0x7FFFFFFFll) return HERO_ERR_ARG;
-  return launch_streaming(quantize_tiles_kernel<T>, blocks, 256, s, (const T*)x, (uint8_t*)q, scale, rows, cols, col_blocks);
+  return launch_kernel(quantize_tiles_kernel<T>, (unsigned)blocks, 256, 0, s, 1, (const T*)x, (uint8_t*)q, scale, rows, cols, col_blocks);
 }
 
 }  // namespace
