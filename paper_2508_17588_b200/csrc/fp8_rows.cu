@@ -403,6 +403,8 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
   HERO_ROWS_CASE(16, 2, LAUNCH) HERO_ROWS_CASE(16, 3, LAUNCH)
 static inline int row_chunks(int D, int piece) { return (D + 32 * piece - 1) / (32 * piece); }
 static inline long long row_ctas(int g, long long rows) { return g == 1 ? (rows + 7) / 8 : rows; }
+// (All of these kernels are placed early, also those of more blocks than fit the chip: they are waited for by nobody while they wait, and a
+// call among others saves the launch, 16.4 -> 14.5 us for the quantiser on 8774 x 3072 bf16.)
 
 template <typename T>
 int gather_ln_f8_dispatch(const void* x, const void* add, const int* idx, const float* shift, const float* scale, int mod_ld, void* out,
