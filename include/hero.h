@@ -269,14 +269,16 @@ int hero_attention_bf16_q_scaled(const void *d_q, const void *d_k, const void *d
  * s = max(amax * fp32(1 / 448), 2^-126) and amax its largest magnitude; q * s is what it stands for.  A block that holds an
  * infinity or a NaN gets a NaN for its scale and for every value.  Columns of e4m3 matrices are a multiple of 16
  * (HERO_ERR_ALIGN otherwise); e4m3 and run-dtype pointers are 16-byte aligned, scales 4-byte.  `dtype` is the run dtype (fp32 or
- * bf16) of the inputs.  Argument errors are reported before anything is launched; no rows at all is HERO_OK.
+ * bf16) of the inputs.  A result shares no byte with an input or with another result, but where hero_rms_norm allows it; rows and
+ * columns are at most 2^31 - 256, and so is what a row of C takes (HERO_ERR_ARG otherwise).  Argument errors are reported before
+ * anything is launched; no rows at all is HERO_OK.
  * hero_gemm_fp8 sets up its status word (a cudaMalloc, see hero_gemm_bf16) on its first call on a device: make that call before any
  * stream capture.  Calls share nothing else, so they may overlap on several streams. */
 
 /* d_x [rows, cols] to d_q and d_scale, blocks of block_rows x 128 (block_rows 1 or 128). */
 int hero_quantize_fp8(const void *d_x, void *d_q, float *d_scale, int rows, int cols, int block_rows, int dtype, void *stream);
 /* hero_gather_ln_modulate with its result as an e4m3 operand: d_out [B,n_sel,D], d_out_scale [B,n_sel,ceil(D/128)].  The other
- * arguments as there; D is at most 12288. */
+ * arguments as there (the list's rows from 0 to N - 1, in any order, a row as often as you like); D is at most 12288. */
 int hero_gather_ln_modulate_fp8(const void *d_x, const void *d_add, const int *d_idx, const float *d_shift, const float *d_scale,
                                 int mod_ld, void *d_out, float *d_out_scale, int B, int N, int n_sel, int D, int dtype, void *stream);
 /* Root-mean-square norm with the residual's addition, for base models whose blocks use it in LayerNorm's place:
@@ -286,7 +288,7 @@ int hero_gather_ln_modulate_fp8(const void *d_x, const void *d_add, const int *d
  * (bf16) or 4 (fp32) and at most 12288; eps is not negative.  A row of zeros with eps = 0 is NaN. */
 int hero_rms_norm(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, int rows, int D, float eps,
                   int dtype, void *stream);
-/* The same with the norm's result as an e4m3 operand (d_out [rows, D] is not d_x or d_add; D is a multiple of 16). */
+/* The same with the norm's result as an e4m3 operand (d_out is neither d_x nor d_add; D is a multiple of 16). */
 int hero_rms_norm_fp8(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, float *d_out_scale, int rows,
                       int D, float eps, int dtype, void *stream);
 /* C[M,N] = act(A[M,K] W[N,K]^T + bias[N]): A with blocks of 1 x 128 (d_a_scale [M,ceil(K/128)]), W with blocks of 128 x 128

@@ -147,7 +147,7 @@ __device__ __forceinline__ void store_f8(uint8_t* row, const float2 (&f)[Piece<T
 // G warps hold a row, V pieces a lane (the last predicated), G growing with the row so that a lane never holds more than three: all
 // its loads are in flight at once, and enough rows are resident.  One row and done: CTAs that stay and fetch the next row ahead took
 // 122 us for 35552 rows of 3072 where these take 114.  Beside the bytes the kernel costs instructions, about as long as the bytes where a
-// row is read once and written in 8 bits: 8774 rows of 3072 bf16 through the norm alone take 16.3 us with packed arithmetic, a scale
+// row is read once and written in 8 bits: 8774 rows of 3072 bf16 through the norm alone take 17 us with packed arithmetic, a scale
 // a warp and no division by the row's length, 20.4 without.
 __host__ __device__ constexpr int rows_threads(int g) { return g == 1 ? 256 : 32 * g; }
 template <int G>
@@ -401,7 +401,7 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
   HERO_ROWS_CASE(4, 2, LAUNCH) HERO_ROWS_CASE(4, 3, LAUNCH)                              \
   HERO_ROWS_CASE(8, 2, LAUNCH) HERO_ROWS_CASE(8, 3, LAUNCH)                              \
   HERO_ROWS_CASE(16, 2, LAUNCH) HERO_ROWS_CASE(16, 3, LAUNCH)
-static inline int row_chunks(int D, int piece) { return (D + 32 * piece - 1) / (32 * piece); }
+static inline int row_chunks(int D, int piece) { return (D - 1) / (32 * piece) + 1; }
 static inline long long row_ctas(int g, long long rows) { return g == 1 ? (rows + 7) / 8 : rows; }
 // (All of these kernels are placed early, also those of more blocks than fit the chip: they are waited for by nobody while they wait, and a
 // call among others saves the launch, 16.4 -> 14.5 us for the quantiser on 8774 x 3072 bf16.)
@@ -413,7 +413,7 @@ int gather_ln_f8_dispatch(const void* x, const void* add, const int* idx, const 
   const int vec = mod_ld % 4 == 0 && aligned16(shift) && aligned16(scale);       // the vectors may be read 16 bytes at a time
   // the same number of CTAs for every batch item, at most as many as stay resident
   auto ctas = [&](int g, int per_sm) {
-    const int need = g == 1 ? (n_sel - 1) / 8 + 1 : n_sel, most = (num_sms() * per_sm + B - 1) / B;
+    const long long need = g == 1 ? (n_sel - 1) / 8 + 1 : n_sel, most = ((long long)num_sms() * per_sm + B - 1) / B;
     return (unsigned)((need < most ? need : most) * B);
   };
 #define HERO_LN_F8(G, V)                                                                                                              \
@@ -523,7 +523,7 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
 
 template <typename T>
 int quantize_t(const void* x, void* q, float* scale, int rows, int cols, int block_rows, cudaStream_t s) {
-  const int col_blocks = (cols + kF8Block - 1) / kF8Block;
+  const int col_blocks = (cols - 1) / kF8Block + 1;
   if (block_rows == 1) {
     const int per_row = row_chunks(cols, Piece<T>::N);
     const long long pieces = (long long)rows * per_row, blocks = (pieces + 7) / 8;

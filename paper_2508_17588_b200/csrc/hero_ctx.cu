@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <new>
 #include <string>
 #include <vector>
@@ -941,13 +942,35 @@ int hero_gemm_bf16(const void* a, const void* w, const void* bias, void* cmat, i
 // ---------------------------------------------------------------- 8-bit operands with a scale for each block of 128
 static bool run_dtype(int dtype) { return dtype == HERO_DTYPE_FP32 || dtype == HERO_DTYPE_BF16; }
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+constexpr int kF8MaxSide = 0x7FFFFF00;       // rows and columns: rounded up to whole tiles they are still an int
+static long long f8_blocks(long long n) { return (n + 127) / 128; }
+// What a call reads or writes (null: nothing), and whether a result shares a byte with an input or another result: thread blocks
+// read while others write.
+struct Span { const void* p; unsigned long long bytes; };
+static bool overlap(const Span& a, const Span& b) {
+  const unsigned long long x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+static bool results_apart(std::initializer_list<Span> results, std::initializer_list<Span> inputs) {
+  for (const Span* r = results.begin(); r != results.end(); ++r) {
+    for (const Span& i : inputs)
+      if (overlap(*r, i)) return false;
+    for (const Span* o = r + 1; o != results.end(); ++o)
+      if (overlap(*r, *o)) return false;
+  }
+  return true;
+}
+static unsigned long long run_bytes(int dtype) { return dtype == HERO_DTYPE_BF16 ? 2 : 4; }
 
 int hero_quantize_fp8(const void* d_x, void* d_q, float* d_scale, int rows, int cols, int block_rows, int dtype, void* stream) {
-  if (rows < 0 || cols <= 0 || (block_rows != 1 && block_rows != 128) || !run_dtype(dtype)) return HERO_ERR_ARG;
+  if (rows < 0 || cols <= 0 || rows > kF8MaxSide || cols > kF8MaxSide || (block_rows != 1 && block_rows != 128) || !run_dtype(dtype))
+    return HERO_ERR_ARG;
   if (cols % 16) return HERO_ERR_ALIGN;
   if (rows == 0) return HERO_OK;
   if (!d_x || !d_q || !d_scale) return HERO_ERR_ARG;
   if (!aligned16(d_x) || !aligned16(d_q) || !aligned4(d_scale)) return HERO_ERR_ALIGN;
+  const unsigned long long n = (unsigned long long)rows * cols, scales = (block_rows == 1 ? rows : f8_blocks(rows)) * f8_blocks(cols);
+  if (!results_apart({{d_q, n}, {d_scale, 4ull * scales}}, {{d_x, n * run_bytes(dtype)}})) return HERO_ERR_ARG;
   return launch_quantize_fp8(d_x, d_q, d_scale, rows, cols, block_rows, dtype, (cudaStream_t)stream);
 }
 
@@ -961,33 +984,44 @@ int hero_gather_ln_modulate_fp8(const void* d_x, const void* d_add, const int* d
   if (!aligned16(d_x) || !aligned16(d_out) || (d_add && !aligned16(d_add)) || !aligned4(d_idx) || !aligned4(d_shift) ||
       !aligned4(d_scale) || !aligned4(d_out_scale))
     return HERO_ERR_ALIGN;
+  const unsigned long long in = (unsigned long long)B * N * D * run_bytes(dtype), sel = (unsigned long long)B * n_sel;
+  const unsigned long long mod = 4 * ((unsigned long long)(B - 1) * mod_ld + D);
+  if (!results_apart({{d_out, sel * D}, {d_out_scale, 4 * sel * f8_blocks(D)}},
+                     {{d_x, in}, {d_add, in}, {d_idx, 4ull * n_sel}, {d_shift, mod}, {d_scale, mod}}))
+    return HERO_ERR_ARG;
   return launch_gather_ln_modulate_fp8(d_x, d_add, d_idx, d_shift, d_scale, mod_ld, d_out, d_out_scale, B, N, n_sel, D, 1e-5f, dtype,
                                        (cudaStream_t)stream);
 }
 
-static int check_rms_norm(const void* x, const void* add, const void* gain, const void* sum, const void* out, int rows, int D, float eps,
-                          int dtype) {
+// x and add may lie under `sum`, and under `out` where both are in the run dtype: a thread reads what it writes over.  (1: launch.)
+static int check_rms_norm(const void* x, const void* add, const void* gain, const void* sum, const void* out, const float* out_scale,
+                          bool f8, int rows, int D, float eps, int dtype) {
   if (rows < 0 || D <= 0 || !(eps >= 0.f) || !run_dtype(dtype)) return HERO_ERR_ARG;
-  if (D % (dtype == HERO_DTYPE_BF16 ? 8 : 4)) return HERO_ERR_ALIGN;
+  if (D % (f8 ? 16 : (dtype == HERO_DTYPE_BF16 ? 8 : 4))) return HERO_ERR_ALIGN;
   if (D > kMaxSmemFloats) return HERO_ERR_ARG;
   if (rows == 0) return HERO_OK;
-  if (!x || !out || sum == out) return HERO_ERR_ARG;
-  if (!aligned16(x) || !aligned16(add) || !aligned16(gain) || !aligned16(sum) || !aligned16(out)) return HERO_ERR_ALIGN;
+  if (!x || !out || f8 != (out_scale != nullptr)) return HERO_ERR_ARG;
+  if (!aligned16(x) || !aligned16(add) || !aligned16(gain) || !aligned16(sum) || !aligned16(out) || !aligned4(out_scale))
+    return HERO_ERR_ALIGN;
+  const unsigned long long n = (unsigned long long)rows * D, bytes = n * run_bytes(dtype);
+  const Span s = {sum, bytes}, o = {out, f8 ? n : bytes}, os = {out_scale, 4ull * rows * f8_blocks(D)}, g = {gain, D * run_bytes(dtype)};
+  if (!results_apart({s, o, os}, {g})) return HERO_ERR_ARG;
+  for (const void* p : {x, add}) {
+    const Span i = {p, bytes};
+    if ((sum != p && overlap(s, i)) || ((f8 || out != p) && overlap(o, i)) || overlap(os, i)) return HERO_ERR_ARG;
+  }
   return 1;
 }
 int hero_rms_norm(const void* d_x, const void* d_add, const void* d_gain, void* d_sum, void* d_out, int rows, int D, float eps, int dtype,
                   void* stream) {
-  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, rows, D, eps, dtype);
+  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, nullptr, false, rows, D, eps, dtype);
   if (r <= 0) return r;
   return launch_rms_norm(d_x, d_add, d_gain, d_sum, d_out, nullptr, rows, D, eps, dtype, (cudaStream_t)stream);
 }
 int hero_rms_norm_fp8(const void* d_x, const void* d_add, const void* d_gain, void* d_sum, void* d_out, float* d_out_scale, int rows,
                       int D, float eps, int dtype, void* stream) {
-  if (D > 0 && D % 16) return HERO_ERR_ALIGN;
-  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, rows, D, eps, dtype);
+  const int r = check_rms_norm(d_x, d_add, d_gain, d_sum, d_out, d_out_scale, true, rows, D, eps, dtype);
   if (r <= 0) return r;
-  if (!d_out_scale || d_out == d_x || d_out == d_add) return HERO_ERR_ARG;
-  if (!aligned4(d_out_scale)) return HERO_ERR_ALIGN;
   return launch_rms_norm(d_x, d_add, d_gain, d_sum, d_out, d_out_scale, rows, D, eps, dtype, (cudaStream_t)stream);
 }
 
@@ -996,12 +1030,19 @@ int hero_gemm_fp8(const void* a, const float* a_scale, const void* w, const floa
   if (M < 0 || N <= 0 || K <= 0 || (act != 0 && act != 1)) return HERO_ERR_ARG;
   if (!run_dtype(out_dtype) && out_dtype != HERO_DTYPE_E4M3) return HERO_ERR_ARG;
   const bool f8 = out_dtype == HERO_DTYPE_E4M3;
+  const unsigned long long row_bytes = f8 ? N : N * run_bytes(out_dtype);
+  if (M > kF8MaxSide || N > kF8MaxSide || K > kF8MaxSide || row_bytes > 0x7FFFFF00ull) return HERO_ERR_ARG;   // (TMA counts a row's bytes)
   if (K % 16 || (f8 && N % 16)) return HERO_ERR_ALIGN;
   if (M == 0) return HERO_OK;
   if (!a || !a_scale || !w || !w_scale || !cmat || f8 != (c_scale != nullptr)) return HERO_ERR_ARG;
   if (!aligned16(a) || !aligned16(w) || !aligned16(cmat) || !aligned4(a_scale) || !aligned4(w_scale) || !aligned4(c_scale) ||
       (reinterpret_cast<uintptr_t>(bias) & 1u))
     return HERO_ERR_ALIGN;
+  const unsigned long long kb = f8_blocks(K), nb = f8_blocks(N);
+  if (!results_apart({{cmat, M * row_bytes}, {c_scale, 4ull * M * nb}},
+                     {{a, (unsigned long long)M * K}, {a_scale, 4ull * M * kb}, {w, (unsigned long long)N * K}, {w_scale, 4 * nb * kb},
+                      {bias, 2ull * N}}))
+    return HERO_ERR_ARG;
   int* st = isolated_status();
   if (!st) return HERO_ERR_NOMEM;
   return launch_tc_gemm_fp8(a, a_scale, w, w_scale, bias, cmat, c_scale, M, N, K, act, out_dtype, st, (cudaStream_t)stream);

@@ -127,6 +127,7 @@ __device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, vo
   }
   *abort_flag = 1;
 }
+
 // ---------------------------------------------------------------- TMA (no multicast anywhere)
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");

@@ -65,6 +65,57 @@ def test_gemm(want, change):
     assert H.load().hero_gemm_fp8(*a.values(), None) == want
 
 
+BIG = 1 << 40                              # (addresses so far apart that nothing of these calls meets)
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=BIG), dict(q=BIG + 496), dict(x=2 * BIG + 240), dict(scale=2 * BIG + 128), dict(scale=BIG + 508), dict(q=3 * BIG - 240)])
+def test_quantize_results_apart(change):
+    a = dict(x=BIG, q=2 * BIG, scale=3 * BIG, rows=4, cols=64, block_rows=1, dtype=1)
+    a.update(change)
+    assert H.load().hero_quantize_fp8(*a.values(), None) == ARG
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("change", [dict(total=P + 128), dict(out=2 * P - 16), dict(total=5 * P + 240), dict(gain=4 * P + 496),
+                                    dict(gain=5 * P - 112), dict(total=2 * P + 16, add=2 * P), dict(add=P + 64, total=P)])
+def test_rms_norm_results_apart(fp8, change):
+    assert _rms(H.load(), fp8, **change) == ARG
+
+
+@pytest.mark.parametrize("change", [dict(scale=P), dict(scale=2 * P + 508), dict(scale=3 * P + 64), dict(scale=4 * P), dict(scale=5 * P + 252),
+                                    dict(out=P + 496)])
+def test_rms_norm_fp8_results_apart(change):
+    assert _rms(H.load(), True, **change) == ARG
+
+
+@pytest.mark.parametrize("change", [
+    dict(out=BIG), dict(out=2 * BIG + 2 * 8 * 64 * 2 - 16), dict(out=3 * BIG), dict(out=4 * BIG + (64 + 64) * 4 - 16), dict(out=5 * BIG),
+    dict(out=7 * BIG - 2 * 4 * 64 + 16), dict(out_scale=BIG + 4), dict(out_scale=3 * BIG + 12)])
+def test_gather_ln_modulate_results_apart(change):
+    a = dict(x=BIG, add=2 * BIG, idx=3 * BIG, shift=4 * BIG, scale=5 * BIG, mod_ld=64, out=6 * BIG, out_scale=7 * BIG, B=2, N=8, n_sel=4, D=64,
+             dtype=1)
+    a.update(change)
+    assert H.load().hero_gather_ln_modulate_fp8(*a.values(), None) == ARG
+
+
+@pytest.mark.parametrize("change", [
+    dict(c=BIG + 240), dict(c=2 * BIG), dict(c=3 * BIG + 32 * 64 - 16), dict(c=4 * BIG), dict(c=5 * BIG + 48), dict(c=7 * BIG - 112),
+    dict(c_scale=BIG), dict(c_scale=2 * BIG + 12), dict(c_scale=3 * BIG), dict(c_scale=5 * BIG)])
+def test_gemm_results_apart(change):
+    a = dict(a=BIG, a_scale=2 * BIG, w=3 * BIG, w_scale=4 * BIG, bias=5 * BIG, c=6 * BIG, c_scale=7 * BIG, M=4, N=32, K=64, act=0, out_dtype=2)
+    a.update(change)
+    assert H.load().hero_gemm_fp8(*a.values(), None) == ARG
+
+
+def test_sizes_that_an_int_does_not_hold_when_rounded_up_to_tiles():
+    lib, top = H.load(), 2 ** 31 - 1
+    assert lib.hero_quantize_fp8(BIG, 2 * BIG, 3 * BIG, top, 16, 128, 1, None) == ARG
+    assert lib.hero_quantize_fp8(BIG, 2 * BIG, 3 * BIG, 1, top - 15, 1, 1, None) == ARG
+    for M, N, K, out in ((top, 1, 16, 1), (1, top, 16, 1), (1, 16, top - 15, 1), (1, 1 << 29, 16, 0), (1, 1 << 30, 16, 1)):
+        assert lib.hero_gemm_fp8(BIG, 2 * BIG, 3 * BIG, 4 * BIG, 0, 5 * BIG, 0, M, N, K, 0, out, None) == ARG
+
+
 def test_the_binding_refuses_what_is_not_on_a_gpu_or_of_another_shape():
     f8, f32 = torch.float8_e4m3fn, torch.float32
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
@@ -92,9 +143,9 @@ def test_the_rule_on_sizes_names_what_there_is():
                 for f8 in (False, True):
                     columns, ctas, swap = H.hero_plan_fp8_gemm(M, N, K, f8)
                     if swap:
-                        assert columns in (16, 32, 64) and ctas in (1, 2, 4, 8)
+                        assert columns == 16 and ctas in (1, 2, 4, 8)
                     elif ctas == 0:
-                        assert columns == 256 or (columns == 128 and not f8)
+                        assert columns == 256
                     else:
                         assert ctas in (1, 2, 4) and (columns == 128 or (columns == 64 and not f8))
                     assert ctas <= -(-K // 128)

@@ -133,6 +133,21 @@ def test_rms_norm_sum_in_place(alias, D):
         check_rms(70, D, dtype, out, True, True, True, alias=alias)
 
 
+def test_rms_norm_sum_and_result_in_place():
+    """sum over one input and, in the run dtype, the result over the other, on rows of one warp and of several."""
+    for D, dtype in ((400, "bf16"), (6144, "fp32")):
+        rng = np.random.default_rng(D)
+        x, add = values(rng, 70, D, dtype, 2.0), values(rng, 70, D, dtype)
+        y = R.rms_norm(x, add, None, 1e-5)[1]
+        total = (torch.from_numpy(x) + torch.from_numpy(add)).to(TORCH[dtype])
+        for over in ("x", "add"):
+            dx, da = to_dev(x, dtype), to_dev(add, dtype)
+            s, o = (dx, da) if over == "x" else (da, dx)
+            H().hero_rms_norm(dx, da, None, s, o, 1e-5)
+            assert torch.equal(s.cpu(), total)
+            assert (np.abs(to_host(o) - y) <= (R.HALF[dtype] + RMS_ERR * 1.01) * np.abs(y) + 1e-37).all()
+
+
 def test_rms_norm_rows_of_zeros_and_rows_that_are_not_finite():
     D = 640
     x = values(np.random.default_rng(1), 6, D, "bf16")
@@ -156,7 +171,7 @@ def test_rms_norm_rows_of_zeros_and_rows_that_are_not_finite():
     ("bf16", 1, 1, 16, 1, False, True, 0), ("bf16", 2, 50, 256, 17, True, True, 0), ("fp32", 1, 40, 128, 9, False, True, 0),
     ("fp32", 2, 33, 272, 33, True, False, 0), ("bf16", 3, 300, 1024, 77, False, True, 0), ("bf16", 2, 123, 2064, 50, True, True, 0),
     ("bf16", 2, 500, 3072, 259, True, True, 0), ("bf16", 1, 40, 4096, 13, True, True, 0), ("fp32", 1, 30, 2048, 30, True, True, 0),
-    ("bf16", 2, 20, 4112, 13, True, True, 0), ("fp32", 2, 20, 2064, 13, False, True, 0),      # rows through shared memory
+    ("bf16", 2, 20, 4112, 13, True, True, 0), ("fp32", 2, 20, 2064, 13, False, True, 0),
     ("bf16", 1, 9, 12288, 9, True, False, 0), ("fp32", 1, 9, 12288, 9, True, False, 0),
     ("bf16", 2, 50, 256, 17, True, True, 1), ("fp32", 2, 50, 144, 17, False, True, 3),        # vectors that are not 16-byte aligned
     ("bf16", 2, 17776, 256, 4387, True, True, 0)])
@@ -190,6 +205,41 @@ def test_gather_ln_modulate_the_same_row_twice():
     q, s = new((1, 4, 512), "e4m3"), new((1, 4, 4), "fp32")
     H().hero_gather_ln_modulate_fp8(to_dev(x[None], "bf16"), None, idx, mod[:, :512], mod[:, 512:], q, s)
     assert torch.equal(q[0, 0].float(), q[0, 1].float()) and torch.equal(s[0, 0], s[0, 3]) and not torch.equal(s[0, 0], s[0, 2])
+
+
+def test_gather_ln_modulate_rows_that_are_not_finite():
+    """NaN for the row that holds one, or an infinity, whatever the modulation; its neighbours and rows off the list as without it."""
+    for D, dtype in ((256, "bf16"), (3072, "bf16"), (1040, "fp32")):
+        x = values(np.random.default_rng(D), 40, D, dtype)
+        bad = x.copy()
+        bad[3, D - 1], bad[5, 0], bad[9, 7] = np.nan, np.inf, -np.inf
+        bad[11:13] = np.nan                                    # not on the list
+        idx = torch.tensor([2, 3, 4, 5, 6, 8, 9, 10, 13], dtype=torch.int32, device="cuda")
+        mod = 0.2 * torch.randn(1, 2 * D, device="cuda", generator=torch.Generator("cuda").manual_seed(D))
+        got = []
+        for v in (x, bad):
+            q, s = new((1, 9, D), "e4m3"), new((1, 9, R.blocks(D)), "fp32")
+            H().hero_gather_ln_modulate_fp8(to_dev(v[None], dtype), None, idx, mod[:, :D], mod[:, D:], q, s)
+            got.append((host32(q[0]), host32(s[0])))
+        hit = np.isin(idx.cpu().numpy(), (3, 5, 9))
+        assert np.isnan(got[1][0][hit]).all() and np.isnan(got[1][1][hit]).all()
+        assert (got[1][0][~hit] == got[0][0][~hit]).all() and (got[1][1][~hit] == got[0][1][~hit]).all()
+
+
+def test_many_small_batch_items():
+    """More items than thread blocks fit the chip, a row or two of each."""
+    B, D = 5000, 144
+    x = values(np.random.default_rng(1), B * 3, D, "bf16").reshape(B, 3, D)
+    mod = torch.from_numpy((0.3 * np.random.default_rng(2).standard_normal((B, 2 * D))).astype(np.float32)).cuda()
+    q, s = new((B, 2, D), "e4m3"), new((B, 2, 2), "fp32")
+    idx = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    xd, h = to_dev(x, "bf16"), H()
+    h.hero_gather_ln_modulate_fp8(xd, None, idx, mod[:, :D], mod[:, D:], q, s)
+    for b in (0, 1, 2500, B - 1):                              # the same rows alone
+        q1, s1 = new((1, 2, D), "e4m3"), new((1, 2, 2), "fp32")
+        h.hero_gather_ln_modulate_fp8(xd[b:b + 1], None, idx, mod[b:b + 1, :D], mod[b:b + 1, D:], q1, s1)
+        assert torch.equal(q[b].float(), q1[0].float()) and torch.equal(s[b], s1[0])
+    assert torch.isfinite(q.float()).all() and torch.isfinite(s).all()
 
 
 # ------------------------------------------------------------------ product
@@ -294,6 +344,52 @@ def test_gemm_leaves_what_is_behind_its_result_alone():
         H().hero_gemm_fp8(*dev, room[:M], None if c_scale is None else c_scale[:M])
         assert torch.isnan(room[M:].float()).all() and torch.isfinite(room[:M].float()).all()
         assert c_scale is None or (torch.isnan(c_scale[M:]).all() and torch.isfinite(c_scale[:M]).all())
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes of input and 2^31 elements: the last rows come out as they do alone."""
+    h, rows, D, last = H(), 700001, 4096, 5
+    g = torch.Generator("cuda").manual_seed(1)
+    x = torch.zeros(rows, D, device="cuda", dtype=torch.bfloat16)
+    x[-200:].normal_(generator=g)
+    tail = x[-last:].clone()
+    # a scale per row, and per 128 x 128: 700001 = 128 * 5468 + 97, the last block by itself
+    for block_rows, n in ((1, last), (128, 97)):
+        q, s = torch.zeros(rows, D, device="cuda", dtype=F8), new((rows if block_rows == 1 else R.blocks(rows), D // 128), "fp32")
+        q1, s1 = new((n, D), "e4m3"), new((n if block_rows == 1 else 1, D // 128), "fp32")
+        h.hero_quantize_fp8(x, q, s, block_rows)
+        h.hero_quantize_fp8(x[-n:].clone(), q1, s1, block_rows)
+        assert torch.equal(q[-n:].view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s[-s1.shape[0]:], s1)
+        assert torch.isfinite(s).all() and (q[:1000].view(torch.uint8) == 0).all()
+    # the norm, its sum over x, and the same in 8 bits
+    o, o1 = torch.empty_like(x), torch.empty_like(tail)
+    h.hero_rms_norm_fp8(x, None, None, None, q, s_rows := new((rows, D // 128), "fp32"))
+    h.hero_rms_norm_fp8(tail, None, None, None, q1[:last], s1 := new((last, D // 128), "fp32"))
+    assert torch.equal(q[-last:].view(torch.uint8), q1[:last].view(torch.uint8)) and torch.equal(s_rows[-last:], s1)
+    h.hero_rms_norm(x, None, None, x, o)
+    h.hero_rms_norm(tail, None, None, None, o1)
+    assert torch.equal(o[-last:], o1) and torch.equal(x[-last:], tail) and (o[:1000] == 0).all()
+    # rows from the end of a long matrix; the second of two items
+    mod = 0.2 * torch.randn(2, 2 * D, device="cuda", generator=g)
+    idx = torch.arange(350000 - last, 350000, dtype=torch.int32, device="cuda")
+    both = x[1:].view(2, 350000, D)
+    q2, s2 = new((2, last, D), "e4m3"), new((2, last, D // 128), "fp32")
+    h.hero_gather_ln_modulate_fp8(both, None, idx, mod[:, :D], mod[:, D:], q2, s2)
+    qa, sa = new((1, last, D), "e4m3"), new((1, last, D // 128), "fp32")
+    h.hero_gather_ln_modulate_fp8(tail[None], None, None, mod[1:, :D], mod[1:, D:], qa, sa)
+    assert torch.equal(q2[1].view(torch.uint8), qa[0].view(torch.uint8)) and torch.equal(s2[1], sa[0])
+    del x, o, both
+    # a product of more than 2^31 results from an operand of more than 2^31 elements: integers, exact in whatever order
+    a = torch.zeros(rows, D, device="cuda", dtype=F8)
+    a[-last:, -128:] = torch.randint(-3, 4, (last, 128), device="cuda", generator=g).float().to(F8)
+    w = torch.randint(-3, 4, (3200, D), device="cuda", generator=g).float().to(F8)
+    ones = lambda *shape: torch.ones(*shape, device="cuda")  # noqa: E731
+    for out in (torch.float32, torch.bfloat16):
+        c = torch.empty(rows, 3200, device="cuda", dtype=out)
+        h.hero_gemm_fp8(a, ones(rows, D // 128), w, ones(25, D // 128), None, c)
+        want = a[-last:, -128:].float().cpu() @ w[:, -128:].float().cpu().t()
+        assert torch.equal(c[-last:].cpu(), want.to(out)) and (c[-1000:-last] == 0).all() and (c[:1000] == 0).all()
+        del c
 
 
 def test_gemm_repeats_bit_for_bit():
