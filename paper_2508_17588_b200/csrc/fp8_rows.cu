@@ -17,40 +17,33 @@ struct Pack;
 template <>
 struct Pack<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& r, float (&f)[4]) {
-    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  static __device__ __forceinline__ void unpack(const uint4& r, float2 (&f)[2]) {
+    f[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y)); f[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
   }
 };
 template <>
 struct Pack<__nv_bfloat16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& r, float (&f)[8]) {
+  static __device__ __forceinline__ void unpack(const uint4& r, float2 (&f)[4]) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&p);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
 };
 
+// A packet to e4m3 (`to`: where it goes).
 template <typename T>
-__device__ __forceinline__ void store_f8(uint8_t* q, const float (&f)[Pack<T>::N], float inv) {      // (q: where the packet goes)
-  const uint32_t a = f8_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-  if constexpr (Pack<T>::N == 8) __stcs(reinterpret_cast<uint2*>(q), make_uint2(a, f8_pack4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)));
-  else __stcs(reinterpret_cast<unsigned int*>(q), a);
+__device__ __forceinline__ void store_f8(uint8_t* to, const float2 (&f)[Pack<T>::N / 2], float inv) {
+  constexpr int N = Pack<T>::N;
+  const float2 i2 = make_float2(inv, inv);
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float2 a = __fmul2_rn(f[2 * i], i2), b = __fmul2_rn(f[2 * i + 1], i2);
+    w[i] = f8_pack4(a.x, a.y, b.x, b.y);
+  }
+  if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(w[0], w[1]));
+  else __stcs(reinterpret_cast<uint32_t*>(to), w[0]);
 }
 
 // Scales of a row's blocks from the magnitudes' bits m[c] that a lane has in its chunk c of 32 lanes (zeros past the end of the row), blocks
@@ -257,13 +250,15 @@ rms_norm_kernel(const T* x, const T* add, const T* __restrict__ gain, T* sum, vo
 // ------------------------------------------------------------------ gather + LayerNorm + modulate
 // G warps take the rows of ONE batch item one after the other, a lane V packets of 16 bytes of each, and with them the item's
 // (1 + scale) and shift of those columns: a thread puts the ones that it needs into shared memory, side by side with its neighbours'
-// (no bank conflicts, and nobody else reads them, so no barrier).  The vectors are twice as long as a bf16 row; 8774 rows of 3072 with a
-// second row to add took 33 us with the vectors read from L1 for every row, 39 with them in registers, which leaves 12 warps an SM, and
-// 32 so.  The next row is on its way while this one is reduced (mean, then squared differences from it) and stored.
+// (no bank conflicts, and nobody else reads them, so no barrier).  The next row is on its way while this one is reduced (mean, then
+// squared differences from it) and stored, and the list is read 32 turns at a time, an entry a lane.  8774 rows of 3072 with a second row
+// to add, from two items: 26.1 us (5.2 TB/s); 31.7 with an entry of the list asked for every turn, for which, or for something that shares its
+// scoreboard, a warp then waited; 33 and 39 (both so) with the vectors read from L1 for every row and with them in registers, which leaves
+// 12 warps an SM.  Bound by instructions, 450 a warp for 24 elements a lane, and the chain of two reductions and a maximum a row.
 __host__ __device__ constexpr int ln_threads(int g) { return g == 1 ? 256 : 32 * g; }
 constexpr int ln_smem(int g, int v, int n) { return v * 2 * n * 4 * ln_threads(g); }
-constexpr int ln_ctas_per_sm(int g, int v, int n) {            // n elements a packet; registers: the row and the next two packets
-  const int regs = 40 + v * (n + 8), warps = ln_threads(g) / 32, by_regs = 64 * 1024 / (32 * warps * ((regs + 7) / 8 * 8));
+constexpr int ln_ctas_per_sm(int g, int v, int n) {            // n elements a packet; registers: the row, the next two packets and the rest
+  const int regs = (g > 1 && v < 3 ? 32 : 40) + v * (n + 8), warps = ln_threads(g) / 32, by_regs = 64 * 1024 / (32 * warps * ((regs + 7) / 8 * 8));
   const int by_smem = 220 * 1024 / (ln_smem(g, v, n) + 1024), by_warps = 64 / warps;
   const int least = by_regs < by_smem ? (by_regs < by_warps ? by_regs : by_warps) : (by_smem < by_warps ? by_smem : by_warps);
   return least < 1 ? 1 : least;
@@ -282,14 +277,17 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
   const int b = blockIdx.x % B, packets = D / N, blocks = (D + kF8Block - 1) / kF8Block;
   const long long first = G == 1 ? (long long)(blockIdx.x / B) * 8 + warp : blockIdx.x / B, step = (long long)(gridDim.x / B) * (G == 1 ? 8 : 1);
   uint4 vx[V], va[V];
-  long long listed = 0;                          // row of x for the row after the fetched one
+  int listed = 0;                                // entries of the list for the next 32 turns, a lane each
   auto look = [&](long long i) {
-    if (i < n_sel) listed = (long long)b * n_rows + (idx ? __ldg(idx + i) : i);
+    const long long mine = i + lane * step;
+    if (mine < n_sel) listed = idx ? __ldg(idx + mine) : (int)mine;
   };
-  auto fetch = [&](long long i) {                // (look(i) came before)
+  auto fetch = [&](long long i, int turn) {
     if (i >= n_sel) return;
-    const uint4* xr = reinterpret_cast<const uint4*>(x + listed * D);
-    const uint4* ar = reinterpret_cast<const uint4*>(add + listed * D);
+    const int entry = __shfl_sync(0xFFFFFFFFu, listed, turn & 31);
+    const long long from = ((long long)b * n_rows + entry) * D;
+    const uint4* xr = reinterpret_cast<const uint4*>(x + from);
+    const uint4* ar = reinterpret_cast<const uint4*>(add + from);
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       const int v = c * 32 * G + t;
@@ -311,8 +309,7 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
     return v;
   };
   look(first);
-  fetch(first);
-  look(first + step);
+  fetch(first, 0);
   const float* sc = scale + (long long)b * mod_ld;
   const float* sh = shift + (long long)b * mod_ld;
 #pragma unroll
@@ -335,34 +332,37 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
       }
     }
   }
+  int turn = 0;
   for (long long i = first; i < n_sel; i += step) {            // (the same turns for a row's threads)
-    float f[V][N];
-    float sum[2] = {0.f, 0.f}, sq[2] = {0.f, 0.f};
+    float2 f[V][N / 2];
+    float2 sum = make_float2(0.f, 0.f), sq = make_float2(0.f, 0.f);
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       P::unpack(vx[c], f[c]);
       if (add) {
-        float a[N];
+        float2 a[N / 2];
         P::unpack(va[c], a);
 #pragma unroll
-        for (int q = 0; q < N; ++q) f[c][q] += a[q];
+        for (int q = 0; q < N / 2; ++q) f[c][q] = __fadd2_rn(f[c][q], a[q]);
       }
 #pragma unroll
-      for (int q = 0; q < N; ++q) sum[q & 1] += f[c][q];
+      for (int q = 0; q < N / 2; ++q) sum = __fadd2_rn(sum, f[c][q]);
     }
-    fetch(i + step);
-    look(i + 2 * step);
-    const float mean = total(make_float2(sum[0], sum[1]), s_part[0]) * inv_d;
+    if ((++turn & 31) == 0) look(i + step);
+    fetch(i + step, turn);
+    const float mean = total(sum, s_part[0]) * inv_d;
+    const float2 neg = make_float2(-mean, -mean);
 #pragma unroll
     for (int c = 0; c < V; ++c)
       if (c * 32 * G + t < packets) {            // (absent packets stay zeros)
 #pragma unroll
-        for (int q = 0; q < N; ++q) {
-          f[c][q] -= mean;
-          sq[q & 1] = fmaf(f[c][q], f[c][q], sq[q & 1]);
+        for (int q = 0; q < N / 2; ++q) {
+          f[c][q] = __fadd2_rn(f[c][q], neg);
+          sq = __ffma2_rn(f[c][q], f[c][q], sq);
         }
       }
-    const float rstd = rsqrtf(fmaf(total(make_float2(sq[0], sq[1]), s_part[1]), inv_d, eps));
+    const float rstd = rsqrtf(fmaf(total(sq, s_part[1]), inv_d, eps));
+    const float2 rstd2 = make_float2(rstd, rstd);
     uint32_t m[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
@@ -371,12 +371,10 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
 #pragma unroll
         for (int q = 0; q < N / 4; ++q) {
           const float4 s4 = s_mod[((c * 2) * (N / 4) + q) * kThreads + threadIdx.x], h4 = s_mod[((c * 2 + 1) * (N / 4) + q) * kThreads + threadIdx.x];
-          float* u = &f[c][4 * q];
-          u[0] = fmaf(u[0] * rstd, s4.x, h4.x);
-          u[1] = fmaf(u[1] * rstd, s4.y, h4.y);
-          u[2] = fmaf(u[2] * rstd, s4.z, h4.z);
-          u[3] = fmaf(u[3] * rstd, s4.w, h4.w);
-          most = max_abs3(max_abs3(most, u[0], u[1]), u[2], u[3]);
+          float2* u = &f[c][2 * q];
+          u[0] = __ffma2_rn(__fmul2_rn(u[0], rstd2), make_float2(s4.x, s4.y), make_float2(h4.x, h4.y));
+          u[1] = __ffma2_rn(__fmul2_rn(u[1], rstd2), make_float2(s4.z, s4.w), make_float2(h4.z, h4.w));
+          most = max_abs3(max_abs3(most, u[0].x, u[0].y), u[1].x, u[1].y);
         }
       }
       m[c] = __float_as_uint(most);
@@ -497,10 +495,10 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
   float m[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    float f[P::N];
+    float2 f[P::N / 2];
     P::unpack(raw[i], f);
 #pragma unroll
-    for (int q = 0; q < P::N; q += 2) m[i & 1] = max_abs3(m[i & 1], f[q], f[q + 1]);
+    for (int q = 0; q < P::N / 2; ++q) m[i & 1] = max_abs3(m[i & 1], f[q].x, f[q].y);
   }
   uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(max_abs3(0.f, m[0], m[1])));
   if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = bits;
@@ -512,7 +510,7 @@ quantize_tiles_kernel(const T* __restrict__ x, uint8_t* __restrict__ out, float*
   for (int i = 0; i < kVec; ++i) {
     const int r = r0 + i * kStep;
     if (r < rows && col < cols) {
-      float f[P::N];
+      float2 f[P::N / 2];
       again(raw[i]);           // (12288 x 3072 bf16: 19.4 us, and 22 with the 64 values kept)
       P::unpack(raw[i], f);
       store_f8<T>(out + (long long)r * cols + col, f, s.inv);

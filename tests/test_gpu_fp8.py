@@ -226,6 +226,25 @@ def test_gather_ln_modulate_rows_that_are_not_finite():
         assert (got[1][0][~hit] == got[0][0][~hit]).all() and (got[1][1][~hit] == got[0][1][~hit]).all()
 
 
+@pytest.mark.parametrize("dtype,B,N,D,n_sel,with_idx", [("bf16", 1, 700000, 16, 600001, True), ("bf16", 2, 31000, 3072, 30007, True),
+                                                        ("fp32", 1, 33000, 2064, 33000, False)])
+def test_gather_ln_modulate_long_lists(dtype, B, N, D, n_sel, with_idx):
+    """Lists so long that a thread block takes more than 32 rows (what it reads of the list at a time): as in calls of a few rows."""
+    g = torch.Generator("cuda").manual_seed(D)
+    x = torch.randn(B, N, D, device="cuda", generator=g).to(TORCH[dtype])
+    mod = 0.3 * torch.randn(B, 2 * D, device="cuda", generator=g)
+    idx = torch.randperm(N, device="cuda", generator=g)[:n_sel].int() if with_idx else None
+    q, s = new((B, n_sel, D), "e4m3"), new((B, n_sel, R.blocks(D)), "fp32")
+    h = H()
+    h.hero_gather_ln_modulate_fp8(x, None, idx, mod[:, :D], mod[:, D:], q, s)
+    rows = torch.arange(n_sel, device="cuda", dtype=torch.int32) if idx is None else idx
+    for at in range(0, n_sel, 5000):
+        part = rows[at:at + 5000].contiguous()
+        q1, s1 = new((B, len(part), D), "e4m3"), new((B, len(part), R.blocks(D)), "fp32")
+        h.hero_gather_ln_modulate_fp8(x, None, part, mod[:, :D], mod[:, D:], q1, s1)
+        assert torch.equal(q[:, at:at + 5000].view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s[:, at:at + 5000], s1)
+
+
 def test_many_small_batch_items():
     """More items than thread blocks fit the chip, a row or two of each."""
     B, D = 5000, 144
