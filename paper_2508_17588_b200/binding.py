@@ -419,6 +419,14 @@ def _f8_call(name: str, device: int, tensors: tuple, args: tuple) -> None:
         raise HeroError(code, name)
 
 
+def _ints(name: str, *values: int) -> tuple:
+    """The values, refused where the C ABI's int would drop their upper bits (ctypes does not tell)."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise HeroError(ERR_ARG, f"{name}: {v} is more than an int holds")
+    return values
+
+
 def _matrix(name: str, arg: str, t, dims: int = 2):
     if t is None or t.dim() != dims:
         raise HeroError(ERR_ARG, f"{name}: {arg} must be a {dims}-dimensional tensor")
@@ -441,7 +449,7 @@ def hero_quantize_fp8(x, q, scale, block_rows: int = 1):
     _f8_call(name, x.get_device(),
              (("x", x, x.dtype, shape), ("q", q, F8, shape),
               ("scale", scale, torch.float32, (rows if block_rows == 1 else _blocks(rows), _blocks(cols)))),
-             (rows, cols, block_rows, dtype))
+             _ints(name, rows, cols, block_rows, dtype))
     return q, scale
 
 
@@ -461,8 +469,8 @@ def hero_gather_ln_modulate_fp8(x, add, idx, shift, scale, out, out_scale):
     # (shift and scale stand between the list and the result in the call: checked above, passed by address)
     _f8_call(name, device,
              (("x", x, x.dtype, shape), ("add", add, x.dtype, shape), ("idx", idx, torch.int32, (n_sel,))),
-             (shift.data_ptr(), scale.data_ptr(), shift.stride(0) if B > 1 else D, *_f8_out(name, device, out, out_scale, (B, n_sel, D)),
-              B, N, n_sel, D, dtype))
+             (shift.data_ptr(), scale.data_ptr(), *_ints(name, shift.stride(0) if B > 1 else D),
+              *_f8_out(name, device, out, out_scale, (B, n_sel, D)), *_ints(name, B, N, n_sel, D, dtype)))
     return out, out_scale
 
 
@@ -482,7 +490,7 @@ def hero_rms_norm(x, add, gain, sum, out, eps: float = 1e-5):
     dt, dtype = x.dtype, _run_dtype(name, x)
     _f8_call(name, x.get_device(),
              (("x", x, dt, shape), ("add", add, dt, shape), ("gain", gain, dt, (D,)), ("sum", sum, dt, shape), ("out", out, dt, shape)),
-             (rows, D, eps, dtype))
+             (*_ints(name, rows, D), eps, dtype))
     return out
 
 
@@ -494,7 +502,7 @@ def hero_rms_norm_fp8(x, add, gain, sum, out, out_scale, eps: float = 1e-5):
     _f8_call(name, x.get_device(),
              (("x", x, dt, shape), ("add", add, dt, shape), ("gain", gain, dt, (D,)), ("sum", sum, dt, shape), ("out", out, F8, shape),
               ("out_scale", out_scale, torch.float32, (rows, _blocks(D)))),
-             (rows, D, eps, dtype))
+             (*_ints(name, rows, D), eps, dtype))
     return out, out_scale
 
 
@@ -516,7 +524,7 @@ def hero_gemm_fp8(a, a_scale, w, w_scale, bias, c, c_scale=None, act: int = 0):
     _f8_call(name, a.get_device(),
              (("a", a, F8, (M, K)), ("a_scale", a_scale, f32, (M, kb)), ("w", w, F8, (N, K)), ("w_scale", w_scale, f32, (nb, kb)),
               ("bias", bias, torch.bfloat16, (N,)), ("c", c, c.dtype, (M, N)), ("c_scale", c_scale, f32, (M, nb))),
-             (M, N, K, act, out))
+             _ints(name, M, N, K, act, out))
     return c
 
 
@@ -538,7 +546,8 @@ def hero_plan_bf16_gemm(M: int, N: int, K: int, qk: bool = False, sms: int = 148
 def hero_plan_fp8_gemm(M: int, N: int, K: int, e4m3_out: bool = False, sms: int = 148):
     """(columns of a tile, thread blocks that share its K, whether W and A have changed places) of the 8-bit GEMM."""
     columns, ctas, swap = C.c_int(), C.c_int(), C.c_int()
-    _check(load().hero_plan_fp8_gemm(M, N, K, int(e4m3_out), sms, C.byref(columns), C.byref(ctas), C.byref(swap)), "hero_plan_fp8_gemm")
+    name = "hero_plan_fp8_gemm"
+    _check(load().hero_plan_fp8_gemm(*_ints(name, M, N, K, int(e4m3_out), sms), C.byref(columns), C.byref(ctas), C.byref(swap)), name)
     return columns.value, ctas.value, bool(swap.value)
 
 
