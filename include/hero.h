@@ -293,7 +293,7 @@ int hero_rms_norm_fp8(const void *d_x, const void *d_add, const void *d_gain, vo
                       int D, float eps, int dtype, void *stream);
 /* C[M,N] = act(A[M,K] W[N,K]^T + bias[N]): A with blocks of 1 x 128 (d_a_scale [M,ceil(K/128)]), W with blocks of 128 x 128
  * (d_w_scale [ceil(N/128),ceil(K/128)]); the sum over a block of 128 on the tensor cores, scaled and added up over the blocks in
- * fp32.  bias is bf16 or NULL; act = 1 applies GELU-tanh.  out_dtype: HERO_DTYPE_BF16, HERO_DTYPE_FP32 (any N; d_c_scale NULL), or
+ * fp32.  bias is bf16 or NULL; act = 1 applies GELU-tanh, in fp32 for every type of result.  out_dtype: HERO_DTYPE_BF16, HERO_DTYPE_FP32 (any N; d_c_scale NULL), or
  * HERO_DTYPE_E4M3 (N a multiple of 16), which writes C as an operand of the next product, d_c_scale [M,ceil(N/128)], quantised from
  * the fp32 result.  Every wait on the device is bounded, as in hero_gemm_bf16; hero_isolated_status reports one that gave up. */
 int hero_gemm_fp8(const void *d_a, const float *d_a_scale, const void *d_w, const float *d_w_scale, const void *d_bias, void *d_c,

@@ -384,18 +384,6 @@ __device__ __forceinline__ void st_global_v8(void* p, const uint32_t* w) {
 }
 
 // ---------------------------------------------------------------- what the GEMMs share
-__device__ __forceinline__ float gelu_tanh_f(float t) {
-  // 0.5 t (1 + tanh(sqrt(2/pi) (t + 0.044715 t^3))) with the hardware tanh (one special-function
-  // instruction, relative error 2^-11: below the bf16 rounding of the result).  The epilogue shares the
-  // SM's power budget with the tensor core, so every instruction saved here is tensor clock gained.
-  const float t2 = t * t;
-  const float u = t * fmaf(0.0356774081f, t2, 0.7978845608f);
-  float th;
-  asm("tanh.approx.f32 %0, %1;" : "=f"(th) : "f"(u));
-  const float h = 0.5f * t;
-  return fmaf(h, th, h);
-}
-
 // Tile order of the persistent pairs.  Consecutive tile numbers run down kGroupM row tiles (of 256) before moving to
 // the next column tile, and only then to the next band of rows: the 74 tiles in flight at any time then cover about
 // 12 x 6 tiles, whose operands stay in L2 and are shared by the pairs working on them, instead of every pair

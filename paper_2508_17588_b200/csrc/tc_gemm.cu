@@ -84,6 +84,18 @@ constexpr int kGemmThreads = 320;                      // producer, issuer, eigh
 constexpr int kEpiWarps = 8;                           // two per TMEM lane quadrant, each with half of a tile's columns
 constexpr size_t kAlignSlack = 1024, kBarrierBytes = 512;
 
+__device__ __forceinline__ float gelu_tanh_f(float t) {
+  // 0.5 t (1 + tanh(sqrt(2/pi) (t + 0.044715 t^3))) with the hardware tanh (one special-function
+  // instruction, relative error 2^-11: below the bf16 rounding of the result).  The epilogue shares the
+  // SM's power budget with the tensor core, so every instruction saved here is tensor clock gained.
+  const float t2 = t * t;
+  const float u = t * fmaf(0.0356774081f, t2, 0.7978845608f);
+  float th;
+  asm("tanh.approx.f32 %0, %1;" : "=f"(th) : "f"(u));
+  const float h = 0.5f * t;
+  return fmaf(h, th, h);
+}
+
 // Where one accumulator row goes.
 struct RowOut {
   bool ok;                 // the row exists

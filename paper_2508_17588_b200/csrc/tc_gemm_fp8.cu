@@ -43,12 +43,13 @@ struct F8Gemm {
   int vec;                       // rows of C start on multiples of: 32, 16 or 0 (less) bytes
 };
 
-// GELU-tanh to fp32 accuracy: t (1 + tanh u) / 2 = t / (1 + exp(-2u)), u = sqrt(2 / pi) (t + 0.044715 t^3).  Four values share one
-// reciprocal, that of the product of their denominators, so that a value costs 1.25 special-function instructions; the exponential
-// is cut off at 2^30 to keep that product finite and t at -16 where it multiplies: a value below -5.1 comes out as something between
-// zero and -16 * 2^-30, less than what fp32 makes of 1 + tanh u there.
-// (bf16 results take the hardware tanh, which is exact enough for their rounding: one special-function instruction.  Scalar
-// arithmetic: packed, the constants take registers that the 128 sums need, and 8774 x 12288 x 3072 454 us for 417.)
+// GELU-tanh to fp32 accuracy, for every type of result: t (1 + tanh u) / 2 = t / (1 + exp(-2u)), u = sqrt(2 / pi) (t + 0.044715 t^3).
+// Four values share one reciprocal, that of the product of their denominators, so that a value costs 1.25 special-function
+// instructions; the exponential is cut off at 2^30 to keep that product finite and t at -16 where it multiplies.  Down to -5.5 a value is
+// off by less than 100 * 2^-24 of itself (30 * 4 roundings of the exponent, and 14 besides); below, where GELU is smaller than
+// 5.2e-9, it comes out between zero and -16 * 2^-30.  (The hardware's tanh, one special-function instruction, does not serve bf16
+// results either: 1 + tanh u cancels below zero, so that its 2^-11 is 20 % of the result at t = -3, and minus infinity becomes NaN.
+// Scalar arithmetic: packed, the constants take registers that the 128 sums need, and 8774 x 12288 x 3072 454 us for 417.)
 __device__ __forceinline__ float gelu_denominator(float t) {
   const float x = t * fmaf(-0.10294324f, t * t, -2.3022082f);        // -2 u log2(e)
   float e;
@@ -60,7 +61,7 @@ __device__ __forceinline__ float gelu_factor(float t) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(t), "f"(-16.f));
   return r;
 }
-__device__ __forceinline__ void gelu_exact4(float2& a, float2& b) {
+__device__ __forceinline__ void gelu4(float2& a, float2& b) {
   const float d0 = gelu_denominator(a.x), d1 = gelu_denominator(a.y), d2 = gelu_denominator(b.x), d3 = gelu_denominator(b.y);
   const float d01 = d0 * d1, d23 = d2 * d3;
   float r;
@@ -69,16 +70,6 @@ __device__ __forceinline__ void gelu_exact4(float2& a, float2& b) {
   a = make_float2(gelu_factor(a.x) * (r01 * d1), gelu_factor(a.y) * (r01 * d0));
   b = make_float2(gelu_factor(b.x) * (r23 * d3), gelu_factor(b.y) * (r23 * d2));
 }
-template <int OUT>
-__device__ __forceinline__ void gelu4(float2& a, float2& b) {
-  if constexpr (OUT == kOutBf16) {
-    a = make_float2(gelu_tanh_f(a.x), gelu_tanh_f(a.y));
-    b = make_float2(gelu_tanh_f(b.x), gelu_tanh_f(b.y));
-  } else {
-    gelu_exact4(a, b);
-  }
-}
-
 // Wait for columns asked for with tmem_ld.  The registers are named behind it, two at a time, so that nothing that uses them moves
 // ahead of the wait.
 template <int CH>
@@ -182,7 +173,7 @@ __device__ __forceinline__ void stage_bias(float* s_bias, const __nv_bfloat16* b
 }
 
 // One row's NC columns: bias and activation.
-template <int NC, int OUT>
+template <int NC>
 __device__ __forceinline__ void finish_row(float2 (&acc)[NC / 2], const float* s_bias, int act) {
 #pragma unroll
   for (int v = 0; v < NC / 4; ++v) {
@@ -192,7 +183,7 @@ __device__ __forceinline__ void finish_row(float2 (&acc)[NC / 2], const float* s
   }
   if (act) {
 #pragma unroll
-    for (int i = 0; i < NC / 2; i += 2) gelu4<OUT>(acc[i], acc[i + 1]);
+    for (int i = 0; i < NC / 2; i += 2) gelu4(acc[i], acc[i + 1]);
   }
 }
 template <int NC>
@@ -317,7 +308,7 @@ template <int NC, int OUT>
 __device__ __forceinline__ void emit_rows(float2 (&acc)[NC / 2], const F8Gemm& g, const float* s_bias, int m, int n0, float* s_rows,
                                           uint32_t* s_amax, uint64_t* meet, int which, volatile int* abort_flag) {
   const int lane = threadIdx.x & 31;
-  finish_row<NC, OUT>(acc, s_bias, g.act);
+  finish_row<NC>(acc, s_bias, g.act);
   if constexpr (OUT == kOutF8) {
     static_assert(2 * NC == kF8Block, "two warps hold a block");
     uint32_t amax = row_amax<NC>(acc);
@@ -338,7 +329,7 @@ __device__ __forceinline__ void emit_rows(float2 (&acc)[NC / 2], const F8Gemm& g
 template <int OUT>
 __device__ __forceinline__ void emit_block(float2 (&acc)[kF8Block / 2], const F8Gemm& g, const CUtensorMap* tm_c, const float* s_bias, int m,
                                            int n0, float* s_rows, int lane) {
-  finish_row<kF8Block, OUT>(acc, s_bias, g.act);
+  finish_row<kF8Block>(acc, s_bias, g.act);
   float inv = 0.f;
   if constexpr (OUT == kOutF8) inv = put_scale(g, row_amax<kF8Block>(acc), m, n0, true);
   if (OUT == kOutF8 || g.vec) store_tma<kF8Block, OUT>(acc, g, tm_c, m - lane, n0, inv, smem_u32(s_rows), lane);
@@ -568,7 +559,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       for (int i = 0; i < BN / 2; ++i) acc[i] = __fadd2_rn(acc[i], make_float2(b, b));
       if (g.act) {
 #pragma unroll
-        for (int i = 0; i < BN / 2; i += 2) gelu4<OUT>(acc[i], acc[i + 1]);
+        for (int i = 0; i < BN / 2; i += 2) gelu4(acc[i], acc[i + 1]);
       }
       F8Scale sc = {};
       if constexpr (OUT == kOutF8) {         // the 128 rows of W are a block: a column's maximum over the four warps
