@@ -397,8 +397,8 @@ gather_ln_f8_kernel(const T* __restrict__ x, const T* __restrict__ add, const in
   HERO_ROWS_CASE(1, 1, LAUNCH) HERO_ROWS_CASE(1, 2, LAUNCH) HERO_ROWS_CASE(1, 3, LAUNCH)  \
   HERO_ROWS_CASE(2, 2, LAUNCH) HERO_ROWS_CASE(2, 3, LAUNCH)                              \
   HERO_ROWS_CASE(4, 2, LAUNCH) HERO_ROWS_CASE(4, 3, LAUNCH)                              \
-  HERO_ROWS_CASE(8, 2, LAUNCH) HERO_ROWS_CASE(8, 3, LAUNCH)                              \
-  HERO_ROWS_CASE(16, 2, LAUNCH) HERO_ROWS_CASE(16, 3, LAUNCH)
+  HERO_ROWS_CASE(8, 2, LAUNCH) HERO_ROWS_CASE(8, 3, LAUNCH)
+#define HERO_ROWS_16(LAUNCH) HERO_ROWS_CASE(16, 2, LAUNCH) HERO_ROWS_CASE(16, 3, LAUNCH)
 static inline int row_chunks(int D, int piece) { return (D - 1) / (32 * piece) + 1; }
 static inline long long row_ctas(int g, long long rows) { return g == 1 ? (rows + 7) / 8 : rows; }
 // (All of these kernels are placed early, also those of more blocks than fit the chip: they are waited for by nobody while they wait, and a
@@ -426,7 +426,8 @@ int gather_ln_f8_dispatch(const void* x, const void* add, const int* idx, const 
   return launch_kernel(gather_ln_f8_kernel<T, G, V>, ctas(G, ln_ctas_per_sm(G, V, Pack<T>::N)), ln_threads(G), smem, s, 1, (const T*)x, \
                        (const T*)add, idx, shift, scale, mod_ld, vec, (uint8_t*)out, out_scale, N, n_sel, B, D, 1.0f / (float)D, eps)
   HERO_ROWS(HERO_LN_F8)
-  HERO_ROWS_CASE(16, 6, HERO_LN_F8)              // (fp32 rows of more than 6144)
+  HERO_ROWS_16(HERO_LN_F8)
+  if constexpr (sizeof(T) == 4) { HERO_ROWS_CASE(16, 6, HERO_LN_F8) }            // rows of more than 6144
 #undef HERO_LN_F8
   return HERO_ERR_ARG;
 }
@@ -439,6 +440,7 @@ int rms_norm_dispatch(const void* x, const void* add, const void* gain, void* su
   return launch_kernel(rms_norm_kernel<T, G, V, Q8>, (unsigned)row_ctas(G, rows), rows_threads(G), 0, s, 1, (const T*)x, (const T*)add,         \
                           (const T*)gain, (T*)sum, out, out_scale, rows, D, 1.0f / (float)D, eps)
   HERO_ROWS(HERO_RMS)
+  if constexpr (sizeof(T) == 4) { HERO_ROWS_16(HERO_RMS) }                       // (12288 columns of bf16 are 8 warps' three pieces)
 #undef HERO_RMS
   return HERO_ERR_ARG;
 }
