@@ -1082,8 +1082,8 @@ int hero_attention_bf16_safe(const void* q, const void* k, const void* v, void* 
 int hero_isolated_status(void* stream) { return poll_isolated_status((cudaStream_t)stream); }
 
 // Self-test of the give-up path: one thread block waits, with a budget of `budget_us` microseconds, on a
-// barrier that nobody will ever complete, through the same bounded-wait helper the tensor-core kernels use;
-// the wait runs out, the block raises the status word and returns.  With a context the word is the
+// barrier that nobody will ever complete, through the bounded-wait helpers that the tensor-core kernels use;
+// the waits run out, the block raises the status word if each of them did, and returns.  With a context the word is the
 // context's (hero_check_status then reports HERO_ERR_TIMEOUT once), and the counters of its attention are left
 // as by a launch whose blocks gave up half way; without one it is the word of the
 // isolated tensor-core calls (hero_isolated_status reports it).

@@ -113,7 +113,8 @@ __device__ __forceinline__ bool mbar_try_wait_at(uint32_t bar, uint32_t parity) 
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                               uint64_t budget_ns = kWaitBudgetNs) {
   if (mbar_try_wait_at(bar, parity)) return;
   uint64_t t0 = 0;
   for (uint32_t it = 1; it < kWaitMaxPolls; ++it) {
@@ -122,7 +123,7 @@ __device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, vo
       if (*abort_flag) return;
       const uint64_t t = global_timer_ns();
       if (t0 == 0) t0 = t;
-      if (t - t0 > kWaitBudgetNs) break;
+      if (t - t0 > budget_ns) break;
     }
   }
   *abort_flag = 1;

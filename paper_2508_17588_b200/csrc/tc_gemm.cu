@@ -687,21 +687,27 @@ tc_gemm_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_cons
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, BN); }
 }
 
-// Self-test of the bounded wait: the barrier below is initialised for one arrival that never comes.
+// Self-test of the bounded waits: the barrier below is initialised for one arrival that never comes.  Two warps wait for it as a warp,
+// a third lane by lane; the status word is raised if both forms gave up and said so.
 __global__ void wait_timeout_selftest_kernel(int* __restrict__ status, unsigned long long budget_ns) {
   __shared__ uint64_t bar;
-  __shared__ int abort_flag;
-  if (threadIdx.x == 0) { mbar_init(&bar, 1); abort_flag = 0; mbar_fence_init(); }
+  __shared__ int abort_flag, abort_lane;
+  __shared__ int warps_gave_up;
+  if (threadIdx.x == 0) { mbar_init(&bar, 1); abort_flag = abort_lane = warps_gave_up = 0; mbar_fence_init(); }
   __syncthreads();
-  const bool ok = mbar_wait_warp(&bar, 0, &abort_flag, budget_ns);
+  if (threadIdx.x < 64) {
+    if (!mbar_wait_warp(&bar, 0, &abort_flag, budget_ns)) warps_gave_up = 1;
+  } else {
+    mbar_wait_lane(smem_u32(&bar), 0, &abort_lane, budget_ns);
+  }
   __syncthreads();
-  if (threadIdx.x == 0 && (!ok || abort_flag)) atomicExch(status, 1);
+  if (threadIdx.x == 0 && abort_flag && warps_gave_up && abort_lane) atomicExch(status, 1);
 }
 
 }  // namespace
 
 int launch_wait_timeout_selftest(int* d_status, int budget_us, cudaStream_t s) {
-  wait_timeout_selftest_kernel<<<1, 64, 0, s>>>(d_status, (unsigned long long)budget_us * 1000ull);
+  wait_timeout_selftest_kernel<<<1, 96, 0, s>>>(d_status, (unsigned long long)budget_us * 1000ull);
   HERO_CUDA_TRY(cudaGetLastError());
   return HERO_OK;
 }
