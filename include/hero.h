@@ -285,17 +285,20 @@ int hero_gather_ln_modulate_fp8(const void *d_x, const void *d_add, const int *d
  * h = x + add, d_sum = h (rounded to dtype), d_out = h / sqrt(mean(h^2) + eps) * gain (of the unrounded h), statistics in fp32.
  * d_x, d_add, d_sum, d_out are [rows, D], d_gain is [D], all in dtype; d_add, d_gain and d_sum may be NULL (nothing added, a gain
  * of 1, the sum not kept).  d_sum may be d_x or d_add, d_out may be d_x or d_add, but not both the same.  D is a multiple of 8
- * (bf16) or 4 (fp32) and at most 12288; eps is not negative.  A row of zeros with eps = 0 is NaN. */
+ * (bf16) or 4 (fp32) and at most 12288; eps is not negative.  A row of zeros with eps = 0 is NaN; a finite row whose sum of squares
+ * passes fp32's range (magnitudes of 1e17 and more) is zeros. */
 int hero_rms_norm(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, int rows, int D, float eps,
                   int dtype, void *stream);
 /* The same with the norm's result as an e4m3 operand (d_out is neither d_x nor d_add; D is a multiple of 16). */
 int hero_rms_norm_fp8(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, float *d_out_scale, int rows,
                       int D, float eps, int dtype, void *stream);
 /* C[M,N] = act(A[M,K] W[N,K]^T + bias[N]): A with blocks of 1 x 128 (d_a_scale [M,ceil(K/128)]), W with blocks of 128 x 128
- * (d_w_scale [ceil(N/128),ceil(K/128)]); the sum over a block of 128 on the tensor cores, scaled and added up over the blocks in
- * fp32.  bias is bf16 or NULL; act = 1 applies GELU-tanh, in fp32 for every type of result.  out_dtype: HERO_DTYPE_BF16, HERO_DTYPE_FP32 (any N; d_c_scale NULL), or
- * HERO_DTYPE_E4M3 (N a multiple of 16), which writes C as an operand of the next product, d_c_scale [M,ceil(N/128)], quantised from
- * the fp32 result.  Every wait on the device is bounded, as in hero_gemm_bf16; hero_isolated_status reports one that gave up. */
+ * (d_w_scale [ceil(N/128),ceil(K/128)]); the sum over a block of 128 on the tensor cores, times the fp32 product of its two scales
+ * and added up over the blocks in fp32.  bias is bf16 or NULL; act = 1 applies GELU-tanh, in fp32 for every type of result (off by
+ * less than 100 * 2^-24 of itself, and below -5.5 between 0 and -2^-26).  out_dtype: HERO_DTYPE_BF16, HERO_DTYPE_FP32 (any N;
+ * d_c_scale NULL), or HERO_DTYPE_E4M3 (N a multiple of 16), which writes C as an operand of the next product, d_c_scale
+ * [M,ceil(N/128)], quantised from the fp32 result.  No gate, no scattered rows and no q/k treatment, which hero_step's products have.
+ * Every wait on the device is bounded, as in hero_gemm_bf16; hero_isolated_status reports one that gave up. */
 int hero_gemm_fp8(const void *d_a, const float *d_a_scale, const void *d_w, const float *d_w_scale, const void *d_bias, void *d_c,
                   float *d_c_scale, int M, int N, int K, int act, int out_dtype, void *stream);
 

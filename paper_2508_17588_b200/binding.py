@@ -397,7 +397,8 @@ def _f8_call(name: str, device: int, tensors: tuple, args: tuple) -> None:
     stream of GPU `device`, which need not be the current one.
 
     Every tensor is contiguous, of its dtype and shape and on that GPU; a HeroError with ERR_ARG says which is not.  (A call of a
-    few microseconds on the GPU is no longer than this function: the checks are the cheapest that torch has.)"""
+    few microseconds on the GPU is no longer than this function: the checks are the cheapest that torch has, and device and stream
+    come from torch._C as plain ints, where the public calls make objects.)"""
     if device < 0:
         raise HeroError(ERR_ARG, f"{name}: tensors must be on a CUDA device")
     ptrs = []

@@ -339,7 +339,8 @@ __device__ __forceinline__ void emit_block(float2 (&acc)[kF8Block / 2], const F8
 // ---------------------------------------------------------------------------------------------------------------
 // One tile per CTA.  A tile is 128 rows of the first operand by BN of the second: of A by W, or (SWAP) of W by A, for
 // few rows of A.  A cluster of `split` CTAs shares a tile, each taking a run of its K blocks; their partial sums meet through
-// distributed shared memory, added in rank order.
+// distributed shared memory: the CTA that finishes a row (a column, SWAP) adds the others' to its own in the order of their ranks, the
+// same order in every call.
 //   warp 0     TMA producer
 //   warp 1     MMA issuer
 //   warps 2..  promotion and epilogue: eight (two per TMEM quadrant, half of the columns each), SWAP: four
@@ -616,7 +617,7 @@ struct PairCfg {
   static constexpr size_t kRowsBytes = (size_t)kWarps * 32 * 33 * 4;     // store_ragged
   static constexpr size_t kSmem = kAlignSlack + (size_t)kStages * kStageBytes + kBiasBytes + kScaleBytes + kRowsBytes + kBarrierBytes;
   // Registers: 384 threads start with 168 each; the first warpgroup gives up what the other two, with 128 sums a thread, take
-  // (128 * 40 + 256 * 232 = 384 * 168).
+  // (128 * 40 + 256 * 232 = 384 * 168).  20 bytes a thread are spilled, 28 with fp32 results.
   static constexpr int kFewRegs = 40, kManyRegs = 232;
   static constexpr int kPromote = 32;                          // columns a TMEM read
 };
