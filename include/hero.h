@@ -286,7 +286,7 @@ int hero_gather_ln_modulate_fp8(const void *d_x, const void *d_add, const int *d
  * d_x, d_add, d_sum, d_out are [rows, D], d_gain is [D], all in dtype; d_add, d_gain and d_sum may be NULL (nothing added, a gain
  * of 1, the sum not kept).  d_sum may be d_x or d_add, d_out may be d_x or d_add, but not both the same.  D is a multiple of 8
  * (bf16) or 4 (fp32) and at most 12288; eps is not negative.  A row of zeros with eps = 0 is NaN; a finite row whose sum of squares
- * passes fp32's range (magnitudes of 1e17 and more) is zeros. */
+ * passes fp32's range (at 12288 columns from magnitudes of 1.6e17 on, at 16 from 4.6e18 on) is zeros. */
 int hero_rms_norm(const void *d_x, const void *d_add, const void *d_gain, void *d_sum, void *d_out, int rows, int D, float eps,
                   int dtype, void *stream);
 /* The same with the norm's result as an e4m3 operand (d_out is neither d_x nor d_add; D is a multiple of 16). */

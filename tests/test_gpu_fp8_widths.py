@@ -69,3 +69,20 @@ def test_rms_norm(dtype, D):
     R.check_quantized(q.float().cpu().numpy(), s.double().cpu().numpy(), y, RMS_ERR * np.abs(y))
     assert (np.abs(to_host(o) - y) <= (R.HALF[dtype] + RMS_ERR * 1.01) * np.abs(y) + 1e-37).all()
     assert torch.equal(total.cpu(), (torch.from_numpy(x) + torch.from_numpy(add)).to(TORCH[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [640, 12288])
+def test_rms_norm_of_large_magnitudes(D, dtype):
+    """Up to the largest whose squares fp32 holds the norm is what it is of ordinary rows; beyond, zeros; the sum is kept all the same."""
+    x = values(np.random.default_rng(D), (5, D), dtype)
+    x[1] = S.round_bf16(np.float32([1e16])) * np.sign(x[1])
+    x[3] = S.round_bf16(np.float32([1e20])) * np.sign(x[3])
+    d, q, s, o, total = to_dev(x, dtype), empty((5, D), F8), empty((5, R.blocks(D))), empty((5, D), TORCH[dtype]), empty((5, D), TORCH[dtype])
+    H().hero_rms_norm_fp8(d, None, None, None, q, s)
+    H().hero_rms_norm(d, None, None, total, o)
+    y = R.rms_norm(x, None, None, 1e-5)[1]
+    y[3] = 0.0
+    R.check_quantized(q.float().cpu().numpy(), s.double().cpu().numpy(), y, RMS_ERR * np.abs(y))
+    assert (np.abs(to_host(o) - y) <= (R.HALF[dtype] + RMS_ERR * 1.01) * np.abs(y) + 1e-37).all()
+    assert torch.equal(total, d)
